@@ -1,4 +1,4 @@
-"""ctypes binding of libzi.so: argument marshalling only, same names as include/zi.h.
+"""ctypes binding of libzi.so: argument marshalling only, same names as include/zi.h and include/zi_fp8.h.
 
 Every step of the path runs in the HIP kernels behind the C ABI.  There is no
 CPU fallback: if the library is missing, loading raises.
@@ -23,6 +23,9 @@ ZI_ERR_IO = -6
 
 ZI_BF16 = 0
 ZI_FP16 = 1
+ZI_FP32 = 2
+ZI_FP8_BLOCK = 128
+ZI_RMS_NORM_MAX_COLS = 65536
 ZI_MODE_ADAMW = 0
 ZI_MODE_ADAM_L2 = 1
 ZI_OPT_SKIP_KERNEL = 0
@@ -36,6 +39,8 @@ EXPORTS = [
     "zi_engine_destroy", "zi_adamw_step_streamed", "zi_engine_last_stats", "zi_engine_set_option",
     "zi_grad_norm_streamed", "zi_adamw_step_files", "zi_engine_file_probe", "zi_engine_link_probe", "zi_plan_chunks", "zi_pinned_alloc", "zi_pinned_free", "zi_hbm_probe",
     "zi_host_grad_norm", "zi_host_adamw_step", "zi_norm_refresh", "zi_plan_step", "zi_grad_norm_noalloc", "zi_grad_offload", "zi_grad_offload_wait", "zi_grad_offload_order", "zi_adamw_step_cpu",
+    "zi_fp8_quantize", "zi_fp8_matmul", "zi_fp8_matmul_workspace_bytes", "zi_rms_norm", "zi_rms_norm_backward",
+    "zi_rms_norm_workspace_bytes",
 ]
 
 
@@ -83,6 +88,24 @@ class zi_chunk_segment(ctypes.Structure):
 class zi_step_plan_item(ctypes.Structure):
     _fields_ = [("tensor", ctypes.c_int32), ("head", ctypes.c_int32), ("n_tiles", ctypes.c_int64),
                 ("first_tile", ctypes.c_int64), ("launch", ctypes.c_int32), ("alone", ctypes.c_int32)]
+
+
+class zi_fp8_matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("scale_ld", ctypes.c_int64), ("block_rows", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class zi_rms_norm_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "gamma", "sum", "y", "rstd")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "x_ld", "residual_ld", "sum_ld", "y_ld")] + \
+               [("eps", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class zi_rms_norm_backward_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dy", "h", "gamma", "rstd", "dsum", "dx", "dgamma")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "dy_ld", "h_ld", "dsum_ld", "dx_ld")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "dgamma_dtype", "accumulate", "reserved")]
 
 
 _lib = None
@@ -179,6 +202,19 @@ def lib() -> ctypes.CDLL:
         L.zi_pinned_alloc.argtypes = [ctypes.POINTER(vp), sz]
         L.zi_pinned_free.restype = ctypes.c_int
         L.zi_pinned_free.argtypes = [vp]
+        fp8 = ctypes.POINTER(zi_fp8_matrix)
+        L.zi_fp8_quantize.restype = ctypes.c_int
+        L.zi_fp8_quantize.argtypes = [vp, i32, i64, i64, i64, fp8, fp8, vp]
+        L.zi_fp8_matmul_workspace_bytes.restype = sz
+        L.zi_fp8_matmul_workspace_bytes.argtypes = [i64, i64, i64]
+        L.zi_fp8_matmul.restype = ctypes.c_int
+        L.zi_fp8_matmul.argtypes = [fp8, fp8, vp, i32, i64, vp, vp, sz, vp]
+        L.zi_rms_norm.restype = ctypes.c_int
+        L.zi_rms_norm.argtypes = [ctypes.POINTER(zi_rms_norm_args), fp8, vp]
+        L.zi_rms_norm_workspace_bytes.restype = sz
+        L.zi_rms_norm_workspace_bytes.argtypes = [i64, i64]
+        L.zi_rms_norm_backward.restype = ctypes.c_int
+        L.zi_rms_norm_backward.argtypes = [ctypes.POINTER(zi_rms_norm_backward_args), vp, sz, vp]
         _lib = L
         _bind_calls(L)
     return _lib
@@ -418,3 +454,89 @@ def zi_pinned_alloc(nbytes: int) -> int:
 
 def zi_pinned_free(ptr) -> int:
     return _check(lib().zi_pinned_free(ptr))
+
+
+# ---- the 8-bit operators of include/zi_fp8.h ------------------------------------------------
+
+def _pitch(x) -> int:
+    """Elements from row to row of a matrix (torch tensor or numpy array) whose columns are neighbours."""
+    if hasattr(x, "data_ptr"):
+        rows, cols, (pitch, step) = *x.shape, x.stride()
+    else:
+        rows, cols, (pitch, step) = *x.shape, (s // x.itemsize for s in x.strides)
+    if step != 1 and cols > 1:
+        raise ValueError("the columns of a matrix have to be neighbours in memory")
+    return int(pitch) if rows > 1 else max(int(pitch), int(cols))
+
+
+def fp8_layout(rows: int, cols: int, block_rows: int = 1):
+    """((rows, ld), (scale rows, scale_ld)): shapes of the two byte arrays that hold a matrix in 8 bits."""
+    up = lambda n, to: -(-n // to) * to                                                   # noqa: E731
+    return (rows, up(cols, ZI_FP8_BLOCK)), (-(-rows // block_rows), up(-(-cols // ZI_FP8_BLOCK), 4))
+
+
+def make_fp8_matrix(data, scale, rows: int, cols: int, block_rows: int = 1, ld: Optional[int] = None,
+                    scale_ld: Optional[int] = None) -> zi_fp8_matrix:
+    """A zi_fp8_matrix over two byte arrays (torch tensors or numpy arrays of two dimensions; addresses with ld and scale_ld)."""
+    return zi_fp8_matrix(_addr(data), _addr(scale), int(rows), int(cols), int(_pitch(data) if ld is None else ld),
+                         int(_pitch(scale) if scale_ld is None else scale_ld), int(block_rows), 0)
+
+
+def _row_pitch(x) -> int:
+    return 0 if x is None else _pitch(x)
+
+
+def make_rms_norm(x, gamma, dtype: int, eps: float, residual=None, sum=None, y=None, rstd=None) -> zi_rms_norm_args:
+    """Arguments of zi_rms_norm from matrices (torch tensors or numpy arrays); None for what is not given or not wanted."""
+    rows, cols = x.shape
+    return zi_rms_norm_args(_addr(x), _addr(residual), _addr(gamma), _addr(sum), _addr(y), _addr(rstd), int(rows), int(cols),
+                            _pitch(x), _row_pitch(residual), _row_pitch(sum), _row_pitch(y), float(eps), int(dtype))
+
+
+def make_rms_norm_backward(dy, h, gamma, rstd, dx, dgamma, dtype: int, dsum=None, dgamma_dtype: Optional[int] = None,
+                           accumulate: bool = False) -> zi_rms_norm_backward_args:
+    """Arguments of zi_rms_norm_backward, as in make_rms_norm; dgamma is of dtype where its type is not given."""
+    rows, cols = dy.shape
+    return zi_rms_norm_backward_args(_addr(dy), _addr(h), _addr(gamma), _addr(rstd), _addr(dsum), _addr(dx), _addr(dgamma),
+                                     int(rows), int(cols), _pitch(dy), _pitch(h), _row_pitch(dsum), _row_pitch(dx), int(dtype),
+                                     int(dtype if dgamma_dtype is None else dgamma_dtype), int(accumulate), 0)
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def _bytes(buffer, given: Optional[int]) -> int:
+    if given is not None:
+        return int(given)
+    return 0 if buffer is None else buffer.numel() * buffer.element_size()
+
+
+def zi_fp8_quantize(x, dtype: int, rows: int, cols: int, ld: int, out: Optional[zi_fp8_matrix] = None,
+                    turned: Optional[zi_fp8_matrix] = None, stream=None) -> int:
+    return _check(lib().zi_fp8_quantize(_addr(x), int(dtype), int(rows), int(cols), int(ld), _ref(out), _ref(turned),
+                                        _stream(stream)))
+
+
+def zi_fp8_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(lib().zi_fp8_matmul_workspace_bytes(int(m), int(n), int(k)))
+
+
+def zi_fp8_matmul(a: zi_fp8_matrix, b: zi_fp8_matrix, d, dtype: int, ldd: int, c=None, d_workspace=None,
+                  workspace_bytes: Optional[int] = None, stream=None) -> int:
+    return _check(lib().zi_fp8_matmul(_ref(a), _ref(b), _addr(d), int(dtype), int(ldd), _addr(c), _addr(d_workspace),
+                                      _bytes(d_workspace, workspace_bytes), _stream(stream)))
+
+
+def zi_rms_norm(args: zi_rms_norm_args, y8: Optional[zi_fp8_matrix] = None, stream=None) -> int:
+    return _check(lib().zi_rms_norm(_ref(args), _ref(y8), _stream(stream)))
+
+
+def zi_rms_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().zi_rms_norm_workspace_bytes(int(rows), int(cols)))
+
+
+def zi_rms_norm_backward(args: zi_rms_norm_backward_args, d_workspace=None, workspace_bytes: Optional[int] = None,
+                         stream=None) -> int:
+    return _check(lib().zi_rms_norm_backward(_ref(args), _addr(d_workspace), _bytes(d_workspace, workspace_bytes),
+                                             _stream(stream)))
