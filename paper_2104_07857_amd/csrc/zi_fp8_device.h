@@ -43,9 +43,10 @@ struct Octet {
         if (valid <= 0) return;
 #pragma unroll
         for (int j = 0; j < 7; ++j) {
-            if (j >= valid) break;
-            if constexpr (DT == ZI_FP32) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
-            else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j % 2));
+            if (j < valid) {
+                if constexpr (DT == ZI_FP32) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+                else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j % 2));
+            }
         }
     }
     __device__ __forceinline__ void store(void* base, int64_t at, int valid) const
@@ -63,9 +64,10 @@ struct Octet {
         }
 #pragma unroll
         for (int j = 0; j < 7; ++j) {
-            if (j >= valid) break;
-            if constexpr (DT == ZI_FP32) reinterpret_cast<uint32_t*>(p)[j] = w[j];
-            else reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+            if (j < valid) {
+                if constexpr (DT == ZI_FP32) reinterpret_cast<uint32_t*>(p)[j] = w[j];
+                else reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+            }
         }
     }
     __device__ __forceinline__ float get(int j) const

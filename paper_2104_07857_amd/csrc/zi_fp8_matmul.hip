@@ -7,8 +7,12 @@
 
 namespace zi {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kStep = kFp8Block;     // of k
+constexpr uint32_t kXcdCount = 8;
 
 // A lane's 32 numbers of a row times those of another, added to what 32 x 32 such pairs have: rows of the first operand are
 // D's columns here, so that a lane's registers hold neighbours of a row of D.
@@ -17,106 +21,302 @@ __device__ __forceinline__ f32x16 multiply_add(i32x8 b, i32x8 a, f32x16 sum, uin
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, sum, 0, 0, 0, (int)b_scale, 0, (int)a_scale);
 }
 
-// Tiles of 128 x 128 and steps of 128 in k, four wavefronts with 64 x 64 each.
-constexpr int kSide = 128, kStep = kFp8Block;
-
-// 16 bytes of a matrix in 8 bits, zeros where it ends.
-__device__ __forceinline__ u32x4 chunk_of(const uint8_t* data, int64_t ld, int64_t rows, int64_t cols, int64_t row, int64_t col)
+// `bytes` leading bytes of 16.
+__device__ __forceinline__ u32x4 leading(u32x4 x, int bytes)
 {
-    u32x4 x = {0, 0, 0, 0};
-    if (row >= rows || col >= cols) return x;
-    x = *reinterpret_cast<const u32x4*>(data + row * ld + col);
-    if (cols - col < 16) {
-        const int valid = (int)(cols - col);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int left = valid - 4 * i;
-            x[i] &= left >= 4 ? 0xFFFFFFFFu : left > 0 ? (1u << (8 * left)) - 1u : 0u;
-        }
+    for (int i = 0; i < 4; ++i) {
+        const int left = bytes - 4 * i;
+        x[i] &= left >= 4 ? 0xFFFFFFFFu : left > 0 ? (1u << (8 * left)) - 1u : 0u;
     }
     return x;
 }
 
-// Chunk p of a row of 128 bytes lies at p ^ (row % 8): lanes that read the same chunk of eight rows reach all banks.
-__device__ __forceinline__ int chunk_at(int row, int p) { return row * kStep + ((p ^ (row & 7)) << 4); }
+// One side of a tile: rows of a matrix in 8 bits from the tile's first one on.  Places are kept as 32-bit offsets from
+// there (launch_fp8_matmul sees to it that they fit).
+struct Side {
+    const uint8_t* data;      // of the tile's first row
+    const uint8_t* scale;     // of its first row of scales
+    uint32_t ld, scale_ld;
+    uint32_t last;            // the matrix' last row, counted from the tile's first
+    uint32_t k;
+    int shift;
+
+    __device__ __forceinline__ Side(const uint8_t* data_, const uint8_t* scale_, int64_t ld_, int64_t scale_ld_, int64_t rows, int64_t row0, int64_t k_, int shift_)
+        : data(data_ + row0 * ld_), scale(scale_ + (row0 >> shift_) * scale_ld_), ld((uint32_t)ld_), scale_ld((uint32_t)scale_ld_),
+          last((uint32_t)(rows - 1 - row0 < 0x7FFFFFFF ? rows - 1 - row0 : 0x7FFFFFFF)), k((uint32_t)k_), shift(shift_)
+    {
+    }
+    __device__ __forceinline__ uint32_t row(uint32_t r) const { return r < last ? r : last; }      // rows past the end are the last one again
+};
+
+__device__ __forceinline__ i32x4 resource(const void* data)
+{
+    const uint64_t at = reinterpret_cast<uint64_t>(data);
+    return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32) & 0xFFFF, -1, 0x00020000};
+}
+
+// 16 or 4 bytes a lane from memory straight to LDS at `lds` (the same in all lanes) + 16 or 4 * lane.  It has no result in registers; whoever reads the LDS
+// waits for it with wait_and_meet().  (m0 is nothing's but this instruction's here.)
+template <int BYTES>
+__device__ __forceinline__ void load_to_lds(i32x4 resource, uint32_t offset, uint32_t more, uint32_t lds)
+{
+    static_assert(BYTES == 16 || BYTES == 4, "");
+    if constexpr (BYTES == 16)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(resource), "s"(more) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(resource), "s"(more) : "memory");
+}
+// All of this wavefront's loads to LDS and reads of it are done, and then all of the workgroup's.
+__device__ __forceinline__ void wait_and_meet()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p)
+{
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+// Tiles are dealt to the XCDs in runs, and a run goes down eight rows of tiles before the next column: the 32 that one XCD has at
+// a time share eight rows' and four columns' operands in its L2.
+constexpr uint32_t kTileRows = 8;
+struct TileOrder {
+    uint32_t across, down, count;
+    __device__ __forceinline__ void place(uint32_t b, uint32_t& tile_m, uint32_t& tile_n) const
+    {
+        const uint32_t x = b % kXcdCount, share = count / kXcdCount, extra = count % kXcdCount;
+        const uint32_t t = x * share + (x < extra ? x : extra) + b / kXcdCount;
+        const uint32_t band = t / (kTileRows * across), in = t - band * kTileRows * across;
+        const uint32_t height = down - band * kTileRows < kTileRows ? down - band * kTileRows : kTileRows;
+        tile_m = band * kTileRows + in % height;
+        tile_n = in / height;
+    }
+};
+
+// Four wavefronts, two by two, with 32 FM x 32 FN of a tile each.  LDS holds two steps of 128 in k; a step's numbers come
+// straight from memory while the step before is multiplied, and a wavefront has half a step in registers while it reads the other half,
+// so that the matrix cores wait for neither: between two barriers there are as many multiplications as reads.
+template <int DT, int FM, int FN>
+__global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(const MatmulArgs p, const TileOrder order)
+{
+    constexpr int kM = 64 * FM, kN = 64 * FN, kStage = (kM + kN) * kStep;
+    __shared__ __align__(128) uint8_t s_stage[2 * kStage];
+    __shared__ __align__(128) uint32_t s_scale[2 * (kM + kN)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int in = lane & 31, half = lane >> 5;
+    uint32_t tile_m, tile_n;
+    order.place(blockIdx.x, tile_m, tile_n);
+    const int64_t m0 = (int64_t)tile_m * kM, n0 = (int64_t)tile_n * kN;
+    const Side a(p.a, p.a_scale, p.a_ld, p.a_scale_ld, p.m, m0, p.k, p.a_shift), b(p.b, p.b_scale, p.b_ld, p.b_scale_ld, p.n, n0, p.k, p.b_shift);
+    const uint32_t wave_m = (uint32_t)(wave >> 1) * 32 * FM, wave_n = (uint32_t)(wave & 1) * 32 * FN;
+
+    // A row of a step is eight chunks of 16 bytes; chunk c of row r lies at c ^ (r % 8), so that lanes that read the same chunk of
+    // eight rows reach all banks.  Eight lanes fetch a row, eight rows a load; the wavefronts take every fourth.
+    uint32_t from_a[2 * FM], from_b[2 * FN];
+    const uint32_t fetch_row = (uint32_t)wave * 8 + (lane >> 3), fetch_chunk = ((lane & 7) ^ (lane >> 3)) * 16u;
+#pragma unroll
+    for (int i = 0; i < 2 * FM; ++i) from_a[i] = a.row(32 * i + fetch_row) * a.ld + fetch_chunk;
+#pragma unroll
+    for (int i = 0; i < 2 * FN; ++i) from_b[i] = b.row(32 * i + fetch_row) * b.ld + fetch_chunk;
+    const i32x4 resource_a = resource(a.data), resource_b = resource(b.data);
+    const uint32_t lds0 = lds_address(s_stage) + (uint32_t)wave * 8 * kStep;
+    const uint32_t steps = (a.k + kStep - 1) / kStep, tail = a.k % kStep;
+
+    const auto fetch = [&](uint32_t step) {
+        const uint32_t stage = (step & 1) * kStage, k0 = step * kStep;
+        if (step + 1 < steps || tail == 0) {
+#pragma unroll
+            for (int i = 0; i < 2 * FM; ++i) load_to_lds<16>(resource_a, from_a[i], k0, lds0 + stage + i * 32 * kStep);
+#pragma unroll
+            for (int i = 0; i < 2 * FN; ++i) load_to_lds<16>(resource_b, from_b[i], k0, lds0 + stage + kM * kStep + i * 32 * kStep);
+            return;
+        }
+        // the last step, which ends inside a block: through registers, zeros behind the end
+        const int valid = (int)tail - (int)fetch_chunk;
+        uint8_t* to = s_stage + stage + ((uint32_t)wave * 64 + lane) * 16;
+        const auto put = [&](const Side& side, int count) {
+#pragma unroll 1
+            for (int i = 0; i < count; ++i, to += 32 * kStep) {
+                const uint32_t at = side.row(32 * i + fetch_row) * side.ld + fetch_chunk;
+                u32x4 x = {0, 0, 0, 0};
+                if (valid > 0) x = leading(*reinterpret_cast<const u32x4*>(side.data + (size_t)at + k0), valid);
+                *reinterpret_cast<u32x4*>(to) = x;
+            }
+        };
+        put(a, 2 * FM);
+        put(b, 2 * FN);
+    };
+
+    // Scales come by fours too: of 64 rows a load, the four bytes of four steps a lane.
+    constexpr int kScaleLoads = (kM + kN) / 64 / 4;
+    uint32_t from_scale[kScaleLoads];
+    i32x4 resource_scale[kScaleLoads];
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const uint32_t first = 64 * (4 * i + (uint32_t)wave);
+        const bool of_a = first < kM;
+        from_scale[i] = of_a ? (a.row(first + lane) >> a.shift) * a.scale_ld : (b.row(first - kM + lane) >> b.shift) * b.scale_ld;
+        resource_scale[i] = resource(of_a ? a.scale : b.scale);
+    }
+    const uint32_t lds_scale0 = lds_address(s_scale) + (uint32_t)wave * 256;
+    const auto fetch_scales = [&](uint32_t step) {
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i)
+            load_to_lds<4>(resource_scale[i], from_scale[i], step, lds_scale0 + (step / 4 & 1) * 4 * (kM + kN) + i * 1024);
+    };
+
+    struct Half {
+        i32x8 a[FM], b[FN];
+    };
+    struct Scales {
+        uint32_t a[FM], b[FN];
+    };
+    const auto read_scales = [&](Scales& f, uint32_t step) {
+        const uint32_t* words = s_scale + (step / 4 & 1) * (kM + kN) + in;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) f.a[i] = words[wave_m + 32 * i] >> (8 * (step % 4));
+#pragma unroll
+        for (int i = 0; i < FN; ++i) f.b[i] = words[kM + wave_n + 32 * i] >> (8 * (step % 4));
+    };
+    const uint32_t read0 = (uint32_t)in * kStep + (((2 * half) ^ (in & 7)) << 4);
+    const auto read = [&](Half& f, uint32_t step, uint32_t h) {
+        const uint32_t stage = (step & 1) * kStage;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t at = (read0 ^ (64 * h) ^ (16 * j)) + stage;
+            const uint8_t *at_a = s_stage + at + wave_m * kStep, *at_b = s_stage + at + (kM + wave_n) * kStep;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const i32x4 x = *reinterpret_cast<const i32x4*>(at_a + i * 32 * kStep);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) f.a[i][4 * j + w] = x[w];
+            }
+#pragma unroll
+            for (int i = 0; i < FN; ++i) {
+                const i32x4 x = *reinterpret_cast<const i32x4*>(at_b + i * 32 * kStep);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) f.b[i][4 * j + w] = x[w];
+            }
+        }
+    };
+    f32x16 sum[FM][FN] = {};
+    const auto multiply = [&](const Half& f, const Scales& scale) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) sum[i][j] = multiply_add(f.b[j], f.a[i], sum[i][j], scale.b[j], scale.a[i]);
+    };
+
+    constexpr int kLdsRead = 0x100, kMatrix = 0x008, kReads = 2 * (FM + FN) / (FM * FN);     // kinds of instruction, and reads for each multiplication
+    if (steps > 0) {
+        Half first, second;
+        Scales scale;
+        fetch(0);
+        fetch_scales(0);
+        wait_and_meet();
+        if (steps > 1) fetch(1);
+        read_scales(scale, 0);
+        read(first, 0, 0);
+        read(second, 0, 1);
+        multiply(first, scale);
+#pragma unroll 1
+        for (uint32_t step = 1; step < steps; ++step) {
+            wait_and_meet();       // this step is there, and the place of the one before is free
+            if (step + 1 < steps) fetch(step + 1);
+            if (step % 4 == 1 && step + 3 < steps) fetch_scales(step + 3);
+            Scales next;
+            read_scales(next, step);
+            read(first, step, 0);
+            multiply(second, scale);
+            scale = next;
+            read(second, step, 1);
+            multiply(first, scale);
+            // every read beside a multiplication of what was read before
+#pragma unroll
+            for (int i = 0; i < 2 * FM * FN; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kLdsRead, kReads, 0);
+                __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+            }
+        }
+        multiply(second, scale);
+    }
+    __syncthreads();               // the places of the steps are used again
+
+    // Of 32 x 32, a lane has row `in` of A and, of B, rows 8 q + 4 half + 0..3 in registers 4 q..4 q + 3.  The tile turns to rows in the LDS, in a
+    // place of the wavefront's own: 16-byte chunk c of row r lies at c ^ (r % kChunks).
+    constexpr int kChunks = 4 * FN, kRows = 32 * FM, kAtOnce = 64 / kChunks;
+    uint8_t* mine = s_stage + wave * (kRows * kChunks * 16);
+    const auto chunk = [&](int r, int c) { return mine + (r * kChunks + (c ^ (r & (kChunks - 1)))) * 16; };
+    const int own_row = lane / kChunks, own_chunk = lane % kChunks;
+    const int64_t col = n0 + wave_n + own_chunk * 8, left = p.n - col;
+    const int valid = left < 8 ? (int)left : 8;
+    const auto turn = [&](auto with_c) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    u32x2* at = reinterpret_cast<u32x2*>(chunk(32 * i + in, 4 * j + q) + 8 * half);
+                    float x[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) x[w] = sum[i][j][4 * q + w];
+                    if constexpr (decltype(with_c)::value) {
+                        Octet<DT> c;
+                        c.w[0] = (*at)[0];
+                        c.w[1] = (*at)[1];
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) x[w] += c.get(w);
+                    }
+                    *at = u32x2{Octet<DT>::pair(x[0], x[1]), Octet<DT>::pair(x[2], x[3])};
+                }
+    };
+    if (p.c) {
+#pragma unroll 4
+        for (int r = own_row; r < kRows; r += kAtOnce) {
+            const int64_t row = m0 + wave_m + r;
+            Octet<DT> c;
+            c.load(p.c, row * p.d_ld + col, row < p.m ? valid : 0);
+            *reinterpret_cast<u32x4*>(chunk(r, own_chunk)) = u32x4{c.w[0], c.w[1], c.w[2], c.w[3]};
+        }
+        turn(std::true_type());
+    } else {
+        turn(std::false_type());
+    }
+#pragma unroll 4
+    for (int r = own_row; r < kRows; r += kAtOnce) {
+        const int64_t row = m0 + wave_m + r;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(chunk(r, own_chunk));
+        Octet<DT> d;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) d.w[w] = x[w];
+        if (row < p.m && valid > 0) d.store(p.d, row * p.d_ld + col, valid);
+    }
+}
+
+template <int DT, int FM, int FN>
+static hipError_t launch_tiles(const MatmulArgs& a, hipStream_t s)
+{
+    TileOrder order;
+    order.across = (uint32_t)((a.n + 64 * FN - 1) / (64 * FN));
+    order.down = (uint32_t)((a.m + 64 * FM - 1) / (64 * FM));
+    order.count = order.across * order.down;
+    hipLaunchKernelGGL((fp8_matmul_kernel<DT, FM, FN>), dim3(order.count), dim3(256), 0, s, a, order);
+    return hipGetLastError();
+}
 
 template <int DT>
-__global__ __launch_bounds__(256) void fp8_matmul_kernel(const MatmulArgs p, uint32_t tiles_across)
+static hipError_t launch_of(const MatmulArgs& a, hipStream_t s)
 {
-    __shared__ __align__(16) uint8_t s_a[kSide * kStep], s_b[kSide * kStep];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int64_t m0 = (int64_t)(blockIdx.x / tiles_across) * kSide, n0 = (int64_t)(blockIdx.x % tiles_across) * kSide;
-    const int wave_m = (wave >> 1) * 64, wave_n = (wave & 1) * 64, in = lane & 31, half = lane >> 5;
-
-    f32x16 sum[2][2] = {};
-    const auto scale_row = [](int64_t row, int64_t rows, int shift) { return (row < rows ? row : rows - 1) >> shift; };
-    const uint8_t *scale_a[2], *scale_b[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        scale_a[i] = p.a_scale + scale_row(m0 + wave_m + 32 * i + in, p.m, p.a_shift) * p.a_scale_ld;
-        scale_b[i] = p.b_scale + scale_row(n0 + wave_n + 32 * i + in, p.n, p.b_shift) * p.b_scale_ld;
-    }
-    for (int64_t k0 = 0; k0 < p.k; k0 += kStep) {
-        const int64_t block = k0 / kStep;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = i * 32 + (t >> 3), part = t & 7;
-            *reinterpret_cast<u32x4*>(s_a + chunk_at(row, part)) = chunk_of(p.a, p.a_ld, p.m, p.k, m0 + row, k0 + part * 16);
-            *reinterpret_cast<u32x4*>(s_b + chunk_at(row, part)) = chunk_of(p.b, p.b_ld, p.n, p.k, n0 + row, k0 + part * 16);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x8 a[2], b[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const u32x4 x = *reinterpret_cast<const u32x4*>(s_a + chunk_at(wave_m + 32 * i + in, 4 * h + 2 * half + j));
-                    const u32x4 y = *reinterpret_cast<const u32x4*>(s_b + chunk_at(wave_n + 32 * i + in, 4 * h + 2 * half + j));
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        a[i][4 * j + w] = (int)x[w];
-                        b[i][4 * j + w] = (int)y[w];
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) sum[i][j] = multiply_add(b[j], a[i], sum[i][j], scale_b[j][block], scale_a[i][block]);
-        }
-    }
-    // Of 32 x 32, a lane has row `in` of A and, of B, rows 8 q + 4 half + 0..3 in registers 4 q..4 q + 3.
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t row = m0 + wave_m + 32 * i + in;
-        if (row >= p.m) continue;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t col = n0 + wave_n + 32 * j + 8 * (r >> 2) + 4 * half + (r & 3);
-                if (col >= p.n) continue;
-                float x = sum[i][j][r];
-                if (p.c) {
-                    Octet<DT> c;
-                    c.w[0] = static_cast<const uint16_t*>(p.c)[row * p.d_ld + col];
-                    x += c.get(0);
-                }
-                static_cast<uint16_t*>(p.d)[row * p.d_ld + col] = (uint16_t)Octet<DT>::pair(x, 0.0f);
-            }
-    }
+    const int64_t large = ((a.m + 255) / 256) * ((a.n + 255) / 256);
+    return large >= 256 ? launch_tiles<DT, 4, 4>(a, s) : launch_tiles<DT, 2, 2>(a, s);
 }
 
 hipError_t launch_fp8_matmul(const MatmulArgs& a, int dtype, float*, hipStream_t s)
 {
-    const uint32_t across = (uint32_t)((a.n + kSide - 1) / kSide);
-    const dim3 grid((unsigned)(across * ((a.m + kSide - 1) / kSide))), block(256);
-    if (dtype == ZI_BF16) hipLaunchKernelGGL(fp8_matmul_kernel<ZI_BF16>, grid, block, 0, s, a, across);
-    else hipLaunchKernelGGL(fp8_matmul_kernel<ZI_FP16>, grid, block, 0, s, a, across);
-    return hipGetLastError();
+    return dtype == ZI_BF16 ? launch_of<ZI_BF16>(a, s) : launch_of<ZI_FP16>(a, s);
 }
 
 }  // namespace zi
