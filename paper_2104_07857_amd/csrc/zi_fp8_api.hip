@@ -9,6 +9,7 @@ using namespace zi::host;
 namespace {
 
 constexpr int64_t kMostRows = (int64_t)1 << 40;     // keeps every product of sizes below 2^63
+constexpr int64_t kMostTiles = (int64_t)1 << 22;    // workgroups of a launch, of up to 1024 threads
 constexpr int64_t kMostPitch = (int64_t)1 << 23;    // of a product's operand: 32-bit offsets reach the 256 rows of a tile
 
 bool bad_real(int32_t dtype, bool fp32) { return dtype != ZI_BF16 && dtype != ZI_FP16 && !(fp32 && dtype == ZI_FP32); }
@@ -171,6 +172,8 @@ extern "C" zi_status zi_fp8_matmul(const zi_fp8_matrix* a, const zi_fp8_matrix* 
     if (zi_status st = check_pitch(ldd, n, "d")) return st;
     if (m > kMostRows / ldd || (k > 0 && (m > kMostRows / a->ld || n > kMostRows / b->ld)))
         return fail(ZI_ERR_UNSUPPORTED, "an operand of more than 2^40 elements");
+    if (up(n, 16) > kMostTiles || up(m, 128) > kMostTiles / up(n, 128))
+        return fail(ZI_ERR_UNSUPPORTED, "D of more than 2^36 elements, or b of more than 2^26 rows");
     if (k > 0 && (a->ld >= kMostPitch || b->ld >= kMostPitch || a->scale_ld >= kMostPitch || b->scale_ld >= kMostPitch))
         return fail(ZI_ERR_UNSUPPORTED, "an operand's pitch is 2^23 or more");
     const size_t wanted = zi_fp8_matmul_workspace_bytes(m, n, k);

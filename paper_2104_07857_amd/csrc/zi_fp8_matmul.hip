@@ -9,6 +9,7 @@ namespace zi {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kStep = kFp8Block;     // of k
@@ -296,6 +297,97 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     }
 }
 
+// ---- few rows -------------------------------------------------------------------------------------------------
+
+// Up to 16 FA rows of A: what counts is how fast B's rows come.  A workgroup has 16 of them, whose k its wavefronts share out in runs of four
+// blocks, W runs at a time, with all of a run's loads in flight at once and its four scales in a word; nothing passes through LDS but the
+// wavefronts' sums, which are added in their order.
+template <int DT, int FA, int W>
+__global__ __launch_bounds__(64 * W) void fp8_matmul_few_kernel(const MatmulArgs p)
+{
+    constexpr int kRun = 4;
+    __shared__ float s_sum[W][FA][16][17];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int in = lane & 15, part = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t row_b = n0 + in < p.n ? n0 + in : p.n - 1;
+    const uint8_t* at_b = p.b + row_b * p.b_ld;
+    const uint8_t* scale_b = p.b_scale + (row_b >> p.b_shift) * p.b_scale_ld;
+    const uint8_t *at_a[FA], *scale_a[FA];
+#pragma unroll
+    for (int f = 0; f < FA; ++f) {
+        const int64_t row = 16 * f + in < p.m ? 16 * f + in : p.m - 1;
+        at_a[f] = p.a + row * p.a_ld;
+        scale_a[f] = p.a_scale + (row >> p.a_shift) * p.a_scale_ld;
+    }
+    f32x4 sum[FA] = {};
+    // A lane's 32 numbers of a block: 16 from each half of it.
+    const auto numbers = [&](const uint8_t* row, int64_t k0, bool whole) {
+        i32x8 x;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t at = k0 + 64 * h + 16 * part;
+            u32x4 v = {0, 0, 0, 0};
+            if (whole) v = *reinterpret_cast<const u32x4*>(row + at);
+            else if (at < p.k) v = leading(*reinterpret_cast<const u32x4*>(row + at), (int)(p.k - at < 16 ? p.k - at : 16));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[4 * h + w] = (int)v[w];
+        }
+        return x;
+    };
+    const auto run_of = [&](int64_t k0, bool whole) {
+        const uint32_t words_b = *reinterpret_cast<const uint32_t*>(scale_b + k0 / kStep);
+        uint32_t words_a[FA];
+        i32x8 b[kRun], a[FA][kRun];
+#pragma unroll
+        for (int f = 0; f < FA; ++f) words_a[f] = *reinterpret_cast<const uint32_t*>(scale_a[f] + k0 / kStep);
+#pragma unroll
+        for (int u = 0; u < kRun; ++u) {
+            b[u] = numbers(at_b, k0 + u * kStep, whole);
+#pragma unroll
+            for (int f = 0; f < FA; ++f) a[f][u] = numbers(at_a[f], k0 + u * kStep, whole);
+        }
+#pragma unroll
+        for (int f = 0; f < FA; ++f) {
+            sum[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[0], a[f][0], sum[f], 0, 0, 0, (int)words_b, 0, (int)words_a[f]);
+            if (whole || k0 + kStep < p.k) sum[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[1], a[f][1], sum[f], 0, 0, 1, (int)words_b, 1, (int)words_a[f]);
+            if (whole || k0 + 2 * kStep < p.k) sum[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[2], a[f][2], sum[f], 0, 0, 2, (int)words_b, 2, (int)words_a[f]);
+            if (whole || k0 + 3 * kStep < p.k) sum[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[3], a[f][3], sum[f], 0, 0, 3, (int)words_b, 3, (int)words_a[f]);
+        }
+    };
+    for (int64_t k0 = (int64_t)wave * kRun * kStep; k0 < p.k; k0 += (int64_t)W * kRun * kStep) {
+        if (k0 + kRun * kStep <= p.k) run_of(k0, true);
+        else run_of(k0, false);          // a scale word may have bytes of no block; what is not there is not multiplied
+    }
+    // A lane has row `in` of A and rows 4 part..4 part + 3 of the 16 of B.
+#pragma unroll
+    for (int f = 0; f < FA; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s_sum[wave][f][in][4 * part + r] = sum[f][r];
+    __syncthreads();
+    for (int i = threadIdx.x; i < FA * 256; i += 64 * W) {
+        const int f = i >> 8, m = (i >> 4) & 15, n = i & 15;
+        const int64_t row = 16 * f + m, col = n0 + n;
+        if (row >= p.m || col >= p.n) continue;
+        float x = s_sum[0][f][m][n];
+#pragma unroll
+        for (int w = 1; w < W; ++w) x += s_sum[w][f][m][n];
+        Octet<DT> y;
+        if (p.c) {
+            y.w[0] = static_cast<const uint16_t*>(p.c)[row * p.d_ld + col];
+            x += y.get(0);
+        }
+        static_cast<uint16_t*>(p.d)[row * p.d_ld + col] = (uint16_t)Octet<DT>::pair(x, 0.0f);
+    }
+}
+
+template <int DT, int FA, int W>
+static hipError_t launch_few(const MatmulArgs& a, hipStream_t s)
+{
+    hipLaunchKernelGGL((fp8_matmul_few_kernel<DT, FA, W>), dim3((unsigned)((a.n + 15) / 16)), dim3(64 * W), 0, s, a);
+    return hipGetLastError();
+}
+
 template <int DT, int FM, int FN>
 static hipError_t launch_tiles(const MatmulArgs& a, hipStream_t s)
 {
@@ -310,6 +402,8 @@ static hipError_t launch_tiles(const MatmulArgs& a, hipStream_t s)
 template <int DT>
 static hipError_t launch_of(const MatmulArgs& a, hipStream_t s)
 {
+    if (a.m <= 16) return launch_few<DT, 1, 8>(a, s);
+    if (a.m <= 32) return launch_few<DT, 2, 8>(a, s);
     const int64_t large = ((a.m + 255) / 256) * ((a.n + 255) / 256);
     return large >= 256 ? launch_tiles<DT, 4, 4>(a, s) : launch_tiles<DT, 2, 2>(a, s);
 }
