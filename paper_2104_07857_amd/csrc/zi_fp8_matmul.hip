@@ -2,6 +2,8 @@
 // block's scale goes in with its numbers, so the sum over k stays in fp32 registers from the first block to the last.
 #include <hip/hip_runtime.h>
 
+#include <utility>
+
 #include "zi_fp8_device.h"
 #include "zi_fp8_internal.h"
 
@@ -75,6 +77,19 @@ __device__ __forceinline__ void wait_and_meet()
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
+// f(number<0>()), ..., f(number<N - 1>())
+template <int I>
+using number = std::integral_constant<int, I>;
+template <typename F, int... I>
+__device__ __forceinline__ void for_each_of(const F& f, std::integer_sequence<int, I...>)
+{
+    (f(number<I>()), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void for_each(const F& f)
+{
+    for_each_of(f, std::make_integer_sequence<int, N>());
+}
 __device__ __forceinline__ uint32_t lds_address(const void* p)
 {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
@@ -113,10 +128,10 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     const Side a(p.a, p.a_scale, p.a_ld, p.a_scale_ld, p.m, m0, p.k, p.a_shift), b(p.b, p.b_scale, p.b_ld, p.b_scale_ld, p.n, n0, p.k, p.b_shift);
     const uint32_t wave_m = (uint32_t)(wave >> 1) * 32 * FM, wave_n = (uint32_t)(wave & 1) * 32 * FN;
 
-    // A row of a step is eight chunks of 16 bytes; chunk c of row r lies at c ^ (r % 8), so that lanes that read the same chunk of
-    // eight rows reach all banks.  Eight lanes fetch a row, eight rows a load; the wavefronts take every fourth.
+    // A row of a step is eight chunks of 16 bytes; chunk c of row r lies at c ^ (r / 2 % 8), so that 16 lanes that read the same chunk of
+    // 16 rows reach all 64 banks.  Eight lanes fetch a row, eight rows a load; the wavefronts take every fourth.
     uint32_t from_a[2 * FM], from_b[2 * FN];
-    const uint32_t fetch_row = (uint32_t)wave * 8 + (lane >> 3), fetch_chunk = ((lane & 7) ^ (lane >> 3)) * 16u;
+    const uint32_t fetch_row = (uint32_t)wave * 8 + (lane >> 3), fetch_chunk = ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) * 16u;
 #pragma unroll
     for (int i = 0; i < 2 * FM; ++i) from_a[i] = a.row(32 * i + fetch_row) * a.ld + fetch_chunk;
 #pragma unroll
@@ -125,24 +140,25 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     const uint32_t lds0 = lds_address(s_stage) + (uint32_t)wave * 8 * kStep;
     const uint32_t steps = (a.k + kStep - 1) / kStep, tail = a.k % kStep;
 
+    const auto fetch_one = [&](auto i, uint32_t step) {
+        const uint32_t to = lds0 + (step & 1) * kStage, k0 = step * kStep;
+        if constexpr (i.value < 2 * FM) load_to_lds<16>(resource_a, from_a[i.value], k0, to + i.value * 32 * kStep);
+        else load_to_lds<16>(resource_b, from_b[i.value - 2 * FM], k0, to + i.value * 32 * kStep);
+    };
     const auto fetch = [&](uint32_t step) {
-        const uint32_t stage = (step & 1) * kStage, k0 = step * kStep;
         if (step + 1 < steps || tail == 0) {
-#pragma unroll
-            for (int i = 0; i < 2 * FM; ++i) load_to_lds<16>(resource_a, from_a[i], k0, lds0 + stage + i * 32 * kStep);
-#pragma unroll
-            for (int i = 0; i < 2 * FN; ++i) load_to_lds<16>(resource_b, from_b[i], k0, lds0 + stage + kM * kStep + i * 32 * kStep);
+            for_each<2 * (FM + FN)>([&](auto i) { fetch_one(i, step); });
             return;
         }
         // the last step, which ends inside a block: through registers, zeros behind the end
         const int valid = (int)tail - (int)fetch_chunk;
-        uint8_t* to = s_stage + stage + ((uint32_t)wave * 64 + lane) * 16;
+        uint8_t* to = s_stage + (step & 1) * kStage + ((uint32_t)wave * 64 + lane) * 16;
         const auto put = [&](const Side& side, int count) {
 #pragma unroll 1
             for (int i = 0; i < count; ++i, to += 32 * kStep) {
                 const uint32_t at = side.row(32 * i + fetch_row) * side.ld + fetch_chunk;
                 u32x4 x = {0, 0, 0, 0};
-                if (valid > 0) x = leading(*reinterpret_cast<const u32x4*>(side.data + (size_t)at + k0), valid);
+                if (valid > 0) x = leading(*reinterpret_cast<const u32x4*>(side.data + (size_t)at + step * kStep), valid);
                 *reinterpret_cast<u32x4*>(to) = x;
             }
         };
@@ -174,74 +190,86 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     struct Scales {
         uint32_t a[FM], b[FN];
     };
+    Scales scale;
     const auto read_scales = [&](Scales& f, uint32_t step) {
         const uint32_t* words = s_scale + (step / 4 & 1) * (kM + kN) + in;
 #pragma unroll
-        for (int i = 0; i < FM; ++i) f.a[i] = words[wave_m + 32 * i] >> (8 * (step % 4));
+        for (int i = 0; i < FM; ++i) f.a[i] = words[wave_m + 32 * i];
 #pragma unroll
-        for (int i = 0; i < FN; ++i) f.b[i] = words[kM + wave_n + 32 * i] >> (8 * (step % 4));
+        for (int i = 0; i < FN; ++i) f.b[i] = words[kM + wave_n + 32 * i];
     };
-    const uint32_t read0 = (uint32_t)in * kStep + (((2 * half) ^ (in & 7)) << 4);
-    const auto read = [&](Half& f, uint32_t step, uint32_t h) {
-        const uint32_t stage = (step & 1) * kStage;
+    const auto take_scales = [&](const Scales& words, uint32_t step) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) scale.a[i] = words.a[i] >> (8 * (step % 4));
+#pragma unroll
+        for (int i = 0; i < FN; ++i) scale.b[i] = words.b[i] >> (8 * (step % 4));
+    };
+    const uint32_t read0 = (uint32_t)in * kStep + (((2 * half) ^ (in / 2 & 7)) << 4);
+    // Number f of the half's FM + FN pieces, in the order that multiply_one() needs them: A's first, all of B's, the rest of A's.
+    const auto read_one = [&](auto f, Half& to, uint32_t step, uint32_t h) {
+        constexpr bool kIsA = f.value == 0 || f.value > FN;
+        constexpr int i = f.value == 0 ? 0 : f.value <= FN ? f.value - 1 : f.value - FN;
+        i32x8& x = kIsA ? to.a[kIsA ? i : 0] : to.b[kIsA ? 0 : i];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const uint32_t at = (read0 ^ (64 * h) ^ (16 * j)) + stage;
-            const uint8_t *at_a = s_stage + at + wave_m * kStep, *at_b = s_stage + at + (kM + wave_n) * kStep;
+            const uint32_t at = (read0 ^ (64 * h) ^ (16 * j)) + (step & 1) * kStage + (kIsA ? wave_m : kM + wave_n) * kStep;
+            const i32x4 y = *reinterpret_cast<const i32x4*>(s_stage + at + i * 32 * kStep);
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const i32x4 x = *reinterpret_cast<const i32x4*>(at_a + i * 32 * kStep);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) f.a[i][4 * j + w] = x[w];
-            }
-#pragma unroll
-            for (int i = 0; i < FN; ++i) {
-                const i32x4 x = *reinterpret_cast<const i32x4*>(at_b + i * 32 * kStep);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) f.b[i][4 * j + w] = x[w];
-            }
+            for (int w = 0; w < 4; ++w) x[4 * j + w] = y[w];
         }
     };
     f32x16 sum[FM][FN] = {};
-    const auto multiply = [&](const Half& f, const Scales& scale) {
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) sum[i][j] = multiply_add(f.b[j], f.a[i], sum[i][j], scale.b[j], scale.a[i]);
+    const auto multiply_one = [&](auto s, const Half& f, const Scales& scale) {
+        constexpr int i = s.value / FN, j = s.value % FN;
+        sum[i][j] = multiply_add(f.b[j], f.a[i], sum[i][j], scale.b[j], scale.a[i]);
+    };
+    // A step: behind the barrier the second half of the step before is multiplied while this one's first half is read, then the first half
+    // while the second is read.  Every multiplication has its share of the reads and loads beside it, in this order: left to itself the
+    // compiler puts reads right in front of what waits for them.
+    constexpr int kSlots = FM * FN, kPieces = FM + FN, kLoads = 2 * (FM + FN);
+    Half first, second;
+    const auto go = [&](uint32_t step, auto loads) {
+        Scales words;
+        read_scales(words, step);
+        for_each<kSlots>([&](auto s) {
+            if constexpr (s.value < kPieces) read_one(s, first, step, 0);
+            if constexpr (decltype(loads)::value)
+                for_each<kLoads / kSlots>([&](auto l) { fetch_one(number<s.value * (kLoads / kSlots) + l.value>(), step + 1); });
+            multiply_one(s, second, scale);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        take_scales(words, step);
+        for_each<kSlots>([&](auto s) {
+            if constexpr (s.value < kPieces) read_one(s, second, step, 1);
+            multiply_one(s, first, scale);
+            __builtin_amdgcn_sched_barrier(0);
+        });
     };
 
-    constexpr int kLdsRead = 0x100, kMatrix = 0x008, kReads = 2 * (FM + FN) / (FM * FN);     // kinds of instruction, and reads for each multiplication
     if (steps > 0) {
-        Half first, second;
-        Scales scale;
         fetch(0);
         fetch_scales(0);
         wait_and_meet();
         if (steps > 1) fetch(1);
         read_scales(scale, 0);
-        read(first, 0, 0);
-        read(second, 0, 1);
-        multiply(first, scale);
+        for_each<kPieces>([&](auto f) { read_one(f, first, 0, 0); });
+        for_each<kPieces>([&](auto f) { read_one(f, second, 0, 1); });
+        for_each<kSlots>([&](auto s) { multiply_one(s, first, scale); });
+        uint32_t step = 1;
 #pragma unroll 1
-        for (uint32_t step = 1; step < steps; ++step) {
+        for (const uint32_t end = tail ? steps - 1 : steps; step + 1 < end; ++step) {
             wait_and_meet();       // this step is there, and the place of the one before is free
+            if (step % 4 == 1 && step + 3 < steps) fetch_scales(step + 3);
+            go(step, std::true_type());
+        }
+#pragma unroll 1
+        for (; step < steps; ++step) {
+            wait_and_meet();
             if (step + 1 < steps) fetch(step + 1);
             if (step % 4 == 1 && step + 3 < steps) fetch_scales(step + 3);
-            Scales next;
-            read_scales(next, step);
-            read(first, step, 0);
-            multiply(second, scale);
-            scale = next;
-            read(second, step, 1);
-            multiply(first, scale);
-            // every read beside a multiplication of what was read before
-#pragma unroll
-            for (int i = 0; i < 2 * FM * FN; ++i) {
-                __builtin_amdgcn_sched_group_barrier(kLdsRead, kReads, 0);
-                __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-            }
+            go(step, std::false_type());
         }
-        multiply(second, scale);
+        for_each<kSlots>([&](auto s) { multiply_one(s, second, scale); });
     }
     __syncthreads();               // the places of the steps are used again
 
