@@ -155,7 +155,12 @@ extern "C" zi_status zi_fp8_quantize(const void* x, int32_t dtype, int64_t rows,
 
 // ---- product --------------------------------------------------------------------------------------------------
 
-extern "C" size_t zi_fp8_matmul_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
+extern "C" size_t zi_fp8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    if (m <= 0 || n <= 0 || k <= 0 || m > kMostRows || n > kMostRows || k > kMostPitch || m > kMostRows / n) return 0;
+    const zi::MatmulPlan plan = zi::plan_fp8_matmul(m, n, k);
+    return plan.parts > 1 ? plan.parts * (size_t)m * (size_t)n * sizeof(float) : 0;
+}
 
 extern "C" zi_status zi_fp8_matmul(const zi_fp8_matrix* a, const zi_fp8_matrix* b, void* d, int32_t dtype, int64_t ldd, const void* c,
                                    void* d_workspace, size_t workspace_bytes, void* hip_stream)

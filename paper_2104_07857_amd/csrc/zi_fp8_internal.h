@@ -46,6 +46,11 @@ struct MatmulArgs {
     int64_t a_ld, b_ld, a_scale_ld, b_scale_ld, d_ld;
     int32_t a_shift, b_shift;     // row >> shift is its row of scales: 0 or 7
 };
+struct MatmulPlan {
+    int shape;               // of the tiles, or -1: the kernel for few rows
+    uint32_t parts, part_steps;      // workgroups that share out k, and their steps of 128
+};
+MatmulPlan plan_fp8_matmul(int64_t m, int64_t n, int64_t k);
 hipError_t launch_fp8_matmul(const MatmulArgs& a, int dtype, float* partials, hipStream_t s);
 
 }  // namespace zi

@@ -2,6 +2,7 @@
 // block's scale goes in with its numbers, so the sum over k stays in fp32 registers from the first block to the last.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <utility>
 
 #include "zi_fp8_device.h"
@@ -70,13 +71,15 @@ __device__ __forceinline__ void load_to_lds(i32x4 resource, uint32_t offset, uin
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(resource), "s"(more) : "memory");
 }
-// All of this wavefront's loads to LDS and reads of it are done, and then all of the workgroup's.
+// All of this wavefront's loads but the last IN_FLIGHT and its reads of LDS are done, and then the whole workgroup's.
+template <int IN_FLIGHT>
 __device__ __forceinline__ void wait_and_meet()
 {
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(IN_FLIGHT) : "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
+
 // f(number<0>()), ..., f(number<N - 1>())
 template <int I>
 using number = std::integral_constant<int, I>;
@@ -99,33 +102,53 @@ __device__ __forceinline__ uint32_t lds_address(const void* p)
 // a time share eight rows' and four columns' operands in its L2.
 constexpr uint32_t kTileRows = 8;
 struct TileOrder {
-    uint32_t across, down, count;
-    __device__ __forceinline__ void place(uint32_t b, uint32_t& tile_m, uint32_t& tile_n) const
+    uint32_t across, down, count;     // tiles, and workgroups
+    uint32_t part_steps;              // where k is shared out, steps of a part
+    __device__ __forceinline__ uint32_t place(uint32_t b, uint32_t& tile_m, uint32_t& tile_n) const
     {
         const uint32_t x = b % kXcdCount, share = count / kXcdCount, extra = count % kXcdCount;
-        const uint32_t t = x * share + (x < extra ? x : extra) + b / kXcdCount;
+        uint32_t t = x * share + (x < extra ? x : extra) + b / kXcdCount;
+        const uint32_t tiles = across * down, part = t / tiles;
+        t -= part * tiles;
         const uint32_t band = t / (kTileRows * across), in = t - band * kTileRows * across;
         const uint32_t height = down - band * kTileRows < kTileRows ? down - band * kTileRows : kTileRows;
         tile_m = band * kTileRows + in % height;
         tile_n = in / height;
+        return part;
     }
 };
 
-// Four wavefronts, two by two, with 32 FM x 32 FN of a tile each.  LDS holds two steps of 128 in k; a step's numbers come
-// straight from memory while the step before is multiplied, and a wavefront has half a step in registers while it reads the other half,
-// so that the matrix cores wait for neither: between two barriers there are as many multiplications as reads.
-template <int DT, int FM, int FN>
-__global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(const MatmulArgs p, const TileOrder order)
+// Up to four floats of a row that ends after `left`.
+__device__ __forceinline__ void put_floats(float* to, const float (&x)[4], int64_t left)
+{
+    if (left >= 4) {
+        *reinterpret_cast<u32x4_of_4*>(to) = u32x4_of_4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+        return;
+    }
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+        if (w < left) to[w] = x[w];
+}
+
+// Four wavefronts, two by two, with 32 FM x 32 FN of a tile each, and steps of a block in k, of which LDS holds RING: while one is
+// multiplied, the loads of the one RING - 1 further on go out, straight from memory to the place of the one before.  A wavefront has half a step in
+// registers while it reads the other half, so that the matrix cores wait for neither.  Where k is shared out over several workgroups
+// (OUT ZI_FP32) each leaves its sums in `partials`.
+template <int OUT, int FM, int FN, int RING>
+__global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_kernel(const MatmulArgs p, const TileOrder order, float* partials)
 {
     constexpr int kM = 64 * FM, kN = 64 * FN, kStage = (kM + kN) * kStep;
-    __shared__ __align__(128) uint8_t s_stage[2 * kStage];
+    __shared__ __align__(128) uint8_t s_stage[RING * kStage];
     __shared__ __align__(128) uint32_t s_scale[2 * (kM + kN)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int in = lane & 31, half = lane >> 5;
     uint32_t tile_m, tile_n;
-    order.place(blockIdx.x, tile_m, tile_n);
+    const uint32_t part = order.place(blockIdx.x, tile_m, tile_n);
     const int64_t m0 = (int64_t)tile_m * kM, n0 = (int64_t)tile_n * kN;
-    const Side a(p.a, p.a_scale, p.a_ld, p.a_scale_ld, p.m, m0, p.k, p.a_shift), b(p.b, p.b_scale, p.b_ld, p.b_scale_ld, p.n, n0, p.k, p.b_shift);
+    const int64_t k0 = OUT == ZI_FP32 ? (int64_t)part * order.part_steps * kStep : 0;
+    const int64_t k = OUT == ZI_FP32 && p.k - k0 > (int64_t)order.part_steps * kStep ? (int64_t)order.part_steps * kStep : p.k - k0;
+    const Side a(p.a + k0, p.a_scale + k0 / kStep, p.a_ld, p.a_scale_ld, p.m, m0, k, p.a_shift);
+    const Side b(p.b + k0, p.b_scale + k0 / kStep, p.b_ld, p.b_scale_ld, p.n, n0, k, p.b_shift);
     const uint32_t wave_m = (uint32_t)(wave >> 1) * 32 * FM, wave_n = (uint32_t)(wave & 1) * 32 * FN;
 
     // A row of a step is eight chunks of 16 bytes; chunk c of row r lies at c ^ (r / 2 % 8), so that 16 lanes that read the same chunk of
@@ -138,21 +161,26 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     for (int i = 0; i < 2 * FN; ++i) from_b[i] = b.row(32 * i + fetch_row) * b.ld + fetch_chunk;
     const i32x4 resource_a = resource(a.data), resource_b = resource(b.data);
     const uint32_t lds0 = lds_address(s_stage) + (uint32_t)wave * 8 * kStep;
-    const uint32_t steps = (a.k + kStep - 1) / kStep, tail = a.k % kStep;
+    const uint32_t steps = (a.k + kStep - 1) / kStep, whole = a.k / kStep;
 
+    // Each XCD begins at another k: where a pitch is a power of two, all of them would else read from the same memory channels at a time (8 x 32768 x 8192
+    // 60.3 / 44.5 us, 4096 x 4096 x 8191 115 / 108); other starts within an XCD lose what its L2 shares.  Groups of four steps, whose scales are one
+    // word, change places.
+    const uint32_t turning = whole / 4 * 4, start = blockIdx.x % kXcdCount * (turning / 4) / kXcdCount * 4;
+    const auto place_of = [&](uint32_t step) { return step >= turning ? step : step + start < turning ? step + start : step + start - turning; };
     const auto fetch_one = [&](auto i, uint32_t step) {
-        const uint32_t to = lds0 + (step & 1) * kStage, k0 = step * kStep;
+        const uint32_t to = lds0 + step % RING * kStage, k0 = place_of(step) * kStep;
         if constexpr (i.value < 2 * FM) load_to_lds<16>(resource_a, from_a[i.value], k0, to + i.value * 32 * kStep);
         else load_to_lds<16>(resource_b, from_b[i.value - 2 * FM], k0, to + i.value * 32 * kStep);
     };
     const auto fetch = [&](uint32_t step) {
-        if (step + 1 < steps || tail == 0) {
+        if (step < whole) {
             for_each<2 * (FM + FN)>([&](auto i) { fetch_one(i, step); });
             return;
         }
         // the last step, which ends inside a block: through registers, zeros behind the end
-        const int valid = (int)tail - (int)fetch_chunk;
-        uint8_t* to = s_stage + (step & 1) * kStage + ((uint32_t)wave * 64 + lane) * 16;
+        const int valid = (int)(a.k % kStep) - (int)fetch_chunk;
+        uint8_t* to = s_stage + step % RING * kStage + ((uint32_t)wave * 64 + lane) * 16;
         const auto put = [&](const Side& side, int count) {
 #pragma unroll 1
             for (int i = 0; i < count; ++i, to += 32 * kStep) {
@@ -167,7 +195,7 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     };
 
     // Scales come by fours too: of 64 rows a load, the four bytes of four steps a lane.
-    constexpr int kScaleLoads = (kM + kN) / 64 / 4;
+    constexpr int kScaleLoads = (FM + FN + 3) / 4;
     uint32_t from_scale[kScaleLoads];
     i32x4 resource_scale[kScaleLoads];
 #pragma unroll
@@ -181,7 +209,7 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     const auto fetch_scales = [&](uint32_t step) {
 #pragma unroll
         for (int i = 0; i < kScaleLoads; ++i)
-            load_to_lds<4>(resource_scale[i], from_scale[i], step, lds_scale0 + (step / 4 & 1) * 4 * (kM + kN) + i * 1024);
+            if (4 * i + wave < FM + FN) load_to_lds<4>(resource_scale[i], from_scale[i], place_of(step), lds_scale0 + (step / 4 & 1) * 4 * (kM + kN) + i * 1024);
     };
 
     struct Half {
@@ -190,7 +218,7 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     struct Scales {
         uint32_t a[FM], b[FN];
     };
-    Scales scale;
+    Scales scale, words;
     const auto read_scales = [&](Scales& f, uint32_t step) {
         const uint32_t* words = s_scale + (step / 4 & 1) * (kM + kN) + in;
 #pragma unroll
@@ -212,7 +240,7 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
         i32x8& x = kIsA ? to.a[kIsA ? i : 0] : to.b[kIsA ? 0 : i];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const uint32_t at = (read0 ^ (64 * h) ^ (16 * j)) + (step & 1) * kStage + (kIsA ? wave_m : kM + wave_n) * kStep;
+            const uint32_t at = (read0 ^ (64 * h) ^ (16 * j)) + step % RING * kStage + (kIsA ? wave_m : kM + wave_n) * kStep;
             const i32x4 y = *reinterpret_cast<const i32x4*>(s_stage + at + i * 32 * kStep);
 #pragma unroll
             for (int w = 0; w < 4; ++w) x[4 * j + w] = y[w];
@@ -227,49 +255,78 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     // while the second is read.  Every multiplication has its share of the reads and loads beside it, in this order: left to itself the
     // compiler puts reads right in front of what waits for them.
     constexpr int kSlots = FM * FN, kPieces = FM + FN, kLoads = 2 * (FM + FN);
+    const auto read_share = [&](auto s, Half& to, uint32_t step, uint32_t h) {     // a piece each, or several where there are more of them
+        constexpr int kEach = (kPieces + kSlots - 1) / kSlots, kFirst = s.value * kEach < kPieces ? s.value * kEach : kPieces;
+        constexpr int kEnd = kFirst + kEach < kPieces ? kFirst + kEach : kPieces;
+        for_each<kEnd - kFirst>([&](auto f) { read_one(number<kFirst + f.value>(), to, step, h); });
+    };
     Half first, second;
     const auto go = [&](uint32_t step, auto loads) {
-        Scales words;
         read_scales(words, step);
         for_each<kSlots>([&](auto s) {
-            if constexpr (s.value < kPieces) read_one(s, first, step, 0);
-            if constexpr (decltype(loads)::value)
-                for_each<kLoads / kSlots>([&](auto l) { fetch_one(number<s.value * (kLoads / kSlots) + l.value>(), step + 1); });
+            read_share(s, first, step, 0);
+            constexpr int kFirst = s.value * kLoads / kSlots, kEnd = (s.value + 1) * kLoads / kSlots;
+            if constexpr (decltype(loads)::value) for_each<kEnd - kFirst>([&](auto l) { fetch_one(number<kFirst + l.value>(), step + RING - 1); });
             multiply_one(s, second, scale);
             __builtin_amdgcn_sched_barrier(0);
         });
         take_scales(words, step);
         for_each<kSlots>([&](auto s) {
-            if constexpr (s.value < kPieces) read_one(s, second, step, 1);
+            read_share(s, second, step, 1);
             multiply_one(s, first, scale);
             __builtin_amdgcn_sched_barrier(0);
         });
     };
 
+    static_assert(RING <= 5, "scales go out three steps ahead, in front of that step's loads");
+    constexpr int kInFlight = (RING - 2) * kLoads;     // loads that may be under way when a step has to be there: those of the steps behind it
     if (steps > 0) {
-        fetch(0);
         fetch_scales(0);
-        wait_and_meet();
-        if (steps > 1) fetch(1);
-        read_scales(scale, 0);
+#pragma unroll 1
+        for (uint32_t step = 0; step < RING - 1 && step < steps; ++step) fetch(step);
+        if (whole >= RING - 1) wait_and_meet<kInFlight>();
+        else wait_and_meet<0>();
+        if (RING - 1 < steps) fetch(RING - 1);
+        read_scales(words, 0);
+        take_scales(words, 0);
         for_each<kPieces>([&](auto f) { read_one(f, first, 0, 0); });
         for_each<kPieces>([&](auto f) { read_one(f, second, 0, 1); });
         for_each<kSlots>([&](auto s) { multiply_one(s, first, scale); });
         uint32_t step = 1;
 #pragma unroll 1
-        for (const uint32_t end = tail ? steps - 1 : steps; step + 1 < end; ++step) {
-            wait_and_meet();       // this step is there, and the place of the one before is free
+        for (; step + RING - 1 < whole; ++step) {
+            wait_and_meet<kInFlight>();       // this step is there, and the place of the one before is free
             if (step % 4 == 1 && step + 3 < steps) fetch_scales(step + 3);
             go(step, std::true_type());
         }
 #pragma unroll 1
         for (; step < steps; ++step) {
-            wait_and_meet();
-            if (step + 1 < steps) fetch(step + 1);
+            wait_and_meet<0>();
+            if (step + RING - 1 < steps) fetch(step + RING - 1);
             if (step % 4 == 1 && step + 3 < steps) fetch_scales(step + 3);
             go(step, std::false_type());
         }
         for_each<kSlots>([&](auto s) { multiply_one(s, second, scale); });
+    }
+    if constexpr (OUT == ZI_FP32) {
+        // Of 32 x 32, a lane has row `in` of A and, of B, rows 8 q + 4 half + 0..3 in registers 4 q..4 q + 3.
+        float* to = partials + (int64_t)part * p.m * p.n;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int64_t row = m0 + wave_m + 32 * i + in;
+            if (row >= p.m) continue;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int64_t col = n0 + wave_n + 32 * j + 8 * q + 4 * half;
+                    float x[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) x[w] = sum[i][j][4 * q + w];
+                    put_floats(to + row * p.n + col, x, p.n - col);
+                }
+        }
+        return;
     }
     __syncthreads();               // the places of the steps are used again
 
@@ -293,20 +350,20 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
 #pragma unroll
                     for (int w = 0; w < 4; ++w) x[w] = sum[i][j][4 * q + w];
                     if constexpr (decltype(with_c)::value) {
-                        Octet<DT> c;
+                        Octet<OUT> c;
                         c.w[0] = (*at)[0];
                         c.w[1] = (*at)[1];
 #pragma unroll
                         for (int w = 0; w < 4; ++w) x[w] += c.get(w);
                     }
-                    *at = u32x2{Octet<DT>::pair(x[0], x[1]), Octet<DT>::pair(x[2], x[3])};
+                    *at = u32x2{Octet<OUT>::pair(x[0], x[1]), Octet<OUT>::pair(x[2], x[3])};
                 }
     };
     if (p.c) {
 #pragma unroll 4
         for (int r = own_row; r < kRows; r += kAtOnce) {
             const int64_t row = m0 + wave_m + r;
-            Octet<DT> c;
+            Octet<OUT> c;
             c.load(p.c, row * p.d_ld + col, row < p.m ? valid : 0);
             *reinterpret_cast<u32x4*>(chunk(r, own_chunk)) = u32x4{c.w[0], c.w[1], c.w[2], c.w[3]};
         }
@@ -318,7 +375,7 @@ __global__ __launch_bounds__(256, FM * FN > 8 ? 1 : 2) void fp8_matmul_kernel(co
     for (int r = own_row; r < kRows; r += kAtOnce) {
         const int64_t row = m0 + wave_m + r;
         const u32x4 x = *reinterpret_cast<const u32x4*>(chunk(r, own_chunk));
-        Octet<DT> d;
+        Octet<OUT> d;
 #pragma unroll
         for (int w = 0; w < 4; ++w) d.w[w] = x[w];
         if (row < p.m && valid > 0) d.store(p.d, row * p.d_ld + col, valid);
@@ -416,29 +473,132 @@ static hipError_t launch_few(const MatmulArgs& a, hipStream_t s)
     return hipGetLastError();
 }
 
-template <int DT, int FM, int FN>
-static hipError_t launch_tiles(const MatmulArgs& a, hipStream_t s)
+// The sums of all parts in their order, and C.
+template <int DT>
+__global__ __launch_bounds__(256) void fp8_matmul_join_kernel(const MatmulArgs p, const float* partials, uint32_t parts, uint32_t across)
+{
+    const int64_t row = blockIdx.x / across, col = ((int64_t)(blockIdx.x % across) * 256 + threadIdx.x) * 4;
+    const int64_t left = p.n - col;
+    if (left <= 0) return;
+    const float* from = partials + row * p.n + col;
+    float x[4] = {};
+    for (uint32_t i = 0; i < parts; ++i, from += p.m * p.n) {
+        if (left >= 4) {
+            const u32x4_of_4 y = *reinterpret_cast<const u32x4_of_4*>(from);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[w] += __uint_as_float(y[w]);
+        } else {
+#pragma unroll
+            for (int w = 0; w < 3; ++w)
+                if (w < left) x[w] += from[w];
+        }
+    }
+    const int64_t at = row * p.d_ld + col;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w >= left) break;
+        if (p.c) {
+            Octet<DT> c;
+            c.w[0] = static_cast<const uint16_t*>(p.c)[at + w];
+            x[w] += c.get(0);
+        }
+        static_cast<uint16_t*>(p.d)[at + w] = (uint16_t)Octet<DT>::pair(x[w], 0.0f);
+    }
+}
+
+// ---- which kernel ---------------------------------------------------------------------------------------------
+
+// Tiles, steps of k in LDS, workgroups that share a compute unit, and what a round of them takes: so much a step and so much besides, in us,
+// measured on the products below, with one workgroup on a compute unit and with two (256 x 256: on up to half of the compute units, and on all of
+// them, where the power the card may draw holds the clock down).  By tile, us:
+//                           64 x 64   64 x 128  128 x 128 (4 steps)  128 x 128 (2)  256 x 256
+//     64 x  4096 x  4096     11.1      12.1         17                 24             -
+//    512 x  4096 x  4096     17.0      15.1         17.6               24.0           35
+//   2048 x  2048 x  2048     17.6      14.3         12.9               15.2           25.6
+//   1001 x  8192 x  2048     32.0      25.4         23.4               19.7           26.7
+//   3000 x  5000 x  4096     99        81           76                 62             54.5
+//   8192 x  8192 x  8192    881       689          628                572            417
+struct TileShape {
+    int rows, cols, together;
+    float step, step_together, besides;
+};
+constexpr int kShapes = 5;
+constexpr TileShape kShape[kShapes] = {{64, 64, 2, 0.25f, 0.40f, 3.5f},
+                                       {64, 128, 2, 0.33f, 0.62f, 4.5f},
+                                       {128, 128, 1, 0.50f, 0.50f, 5.0f},
+                                       {128, 128, 2, 0.70f, 0.95f, 5.5f},
+                                       {256, 256, 1, 1.05f, 1.60f, 10.0f}};
+constexpr int64_t kUnits = 256;                  // compute units
+constexpr float kStream = 6.0e6f, kFewStream = 4.7e6f, kJoinStream = 3.0e6f, kJoin = 3.0f, kFewBesides = 3.0f;      // bytes a us; us
+
+// The least of these estimates: a kernel for few rows of A, where it reads B at 4.7 TB/s (2.9 us for 1 x 1024 x 1024 and 5.1 for 1 x 4096 x 4096, tiles
+// 5.3 and 8.7; but 13.5 for 1 x 16384 x 4096, tiles 11.9), or tiles, and of the smallest as many parts of k as pay for adding them (13 x 4096 x
+// 16384 in one, two, four, eight parts 35.1, 22.0, 15.3, 16.8).
+MatmulPlan plan_fp8_matmul(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t steps = (k + kStep - 1) / kStep;
+    const float stream = ((float)m + (float)n) * (float)k;
+    MatmulPlan best{-1, 1, (uint32_t)((steps + 3) / 4 * 4)};
+    float least = INFINITY;
+    if (m <= 32) least = kFewBesides + (m <= 16 ? 1.0f : 1.25f) * stream / kFewStream;
+    for (int i = 0; i < kShapes; ++i) {
+        const TileShape& t = kShape[i];
+        const int64_t tiles = ((m + t.rows - 1) / t.rows) * ((n + t.cols - 1) / t.cols);
+        for (int64_t parts = 1; parts <= (i == 0 ? 16 : 1); parts *= 2) {
+            const int64_t each = ((steps + parts - 1) / parts + 3) / 4 * 4;       // a part begins with a word of scales
+            const int64_t really = each ? (steps + each - 1) / each : 1;
+            const int64_t groups = tiles * really, rounds = groups / (kUnits * t.together), rest = groups % (kUnits * t.together);
+            const auto round = [&](float step) { return (float)(really > 1 ? each : steps) * step + t.besides; };
+            const bool apart = t.together == 2 ? rest <= kUnits : rounds == 0 && rest <= kUnits / 2;
+            const float work = (float)rounds * round(t.step_together) + (rest ? round(apart ? t.step : t.step_together) : 0.0f);
+            float all = 0.01f * work + (work > stream / kStream ? work : stream / kStream);
+            if (really > 1) all += kJoin + 8.0f * (float)really * (float)m * (float)n / kJoinStream;
+            if (all < least) {
+                least = all;
+                best = {i, (uint32_t)really, (uint32_t)each};
+            }
+        }
+    }
+    return best;
+}
+
+template <int DT, int FM, int FN, int RING>
+static hipError_t launch_tiles(const MatmulArgs& a, const MatmulPlan& plan, float* partials, hipStream_t s)
 {
     TileOrder order;
     order.across = (uint32_t)((a.n + 64 * FN - 1) / (64 * FN));
     order.down = (uint32_t)((a.m + 64 * FM - 1) / (64 * FM));
-    order.count = order.across * order.down;
-    hipLaunchKernelGGL((fp8_matmul_kernel<DT, FM, FN>), dim3(order.count), dim3(256), 0, s, a, order);
+    order.count = order.across * order.down * plan.parts;
+    order.part_steps = plan.part_steps;
+    if constexpr (FM == 1 && FN == 1) {
+        if (plan.parts > 1) {
+            hipLaunchKernelGGL((fp8_matmul_kernel<ZI_FP32, FM, FN, RING>), dim3(order.count), dim3(256), 0, s, a, order, partials);
+            const uint32_t across = (uint32_t)((a.n + 1023) / 1024);
+            hipLaunchKernelGGL(fp8_matmul_join_kernel<DT>, dim3((unsigned)(across * a.m)), dim3(256), 0, s, a, (const float*)partials, plan.parts, across);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((fp8_matmul_kernel<DT, FM, FN, RING>), dim3(order.count), dim3(256), 0, s, a, order, (float*)nullptr);
     return hipGetLastError();
 }
 
 template <int DT>
-static hipError_t launch_of(const MatmulArgs& a, hipStream_t s)
+static hipError_t launch_of(const MatmulArgs& a, float* partials, hipStream_t s)
 {
-    if (a.m <= 16) return launch_few<DT, 1, 8>(a, s);
-    if (a.m <= 32) return launch_few<DT, 2, 8>(a, s);
-    const int64_t large = ((a.m + 255) / 256) * ((a.n + 255) / 256);
-    return large >= 256 ? launch_tiles<DT, 4, 4>(a, s) : launch_tiles<DT, 2, 2>(a, s);
+    const MatmulPlan plan = plan_fp8_matmul(a.m, a.n, a.k);
+    switch (plan.shape) {
+    case 0: return launch_tiles<DT, 1, 1, 4>(a, plan, partials, s);
+    case 1: return launch_tiles<DT, 1, 2, 3>(a, plan, partials, s);
+    case 2: return launch_tiles<DT, 2, 2, 4>(a, plan, partials, s);
+    case 3: return launch_tiles<DT, 2, 2, 2>(a, plan, partials, s);
+    case 4: return launch_tiles<DT, 4, 4, 2>(a, plan, partials, s);
+    }
+    return a.m <= 16 ? launch_few<DT, 1, 8>(a, s) : launch_few<DT, 2, 8>(a, s);
 }
 
-hipError_t launch_fp8_matmul(const MatmulArgs& a, int dtype, float*, hipStream_t s)
+hipError_t launch_fp8_matmul(const MatmulArgs& a, int dtype, float* partials, hipStream_t s)
 {
-    return dtype == ZI_BF16 ? launch_of<ZI_BF16>(a, s) : launch_of<ZI_FP16>(a, s);
+    return dtype == ZI_BF16 ? launch_of<ZI_BF16>(a, partials, s) : launch_of<ZI_FP16>(a, partials, s);
 }
 
 }  // namespace zi

@@ -101,6 +101,22 @@ def test_matmul_refuses():
     _refused(INVALID, "pitch of d", f, a, b, d, BF16, 5)
     _refused(INVALID, "overlap", f, a, b, a.data, BF16, 6)
     _refused(INVALID, "overlap", f, a, b, d, BF16, 6, c=d.ctypes.data + 2)
+    _refused(UNSUPPORTED, "pitch", f, _matrix(4, 100, ld=1 << 23), b, d, BF16, 6)
+    _refused(UNSUPPORTED, "2^26", f, _matrix(4, 16), _matrix(4, 16, rows=1 << 27), d, BF16, 1 << 27)
+
+
+def test_matmul_workspace():
+    """What is asked for has to be there; where k is not shared out nothing is."""
+    m, n, k = 64, 128, 16384
+    nbytes = zi.zi_fp8_matmul_workspace_bytes(m, n, k)
+    assert nbytes > 0 and nbytes % (m * n * 4) == 0
+    assert zi.zi_fp8_matmul_workspace_bytes(4096, 4096, 4096) == 0 == zi.zi_fp8_matmul_workspace_bytes(0, n, k) == zi.zi_fp8_matmul_workspace_bytes(m, n, 0)
+    a, b, d, ws = _matrix(m, k), _matrix(n, k, 128), _half(m, n), _bytes(nbytes)
+    f = zi.zi_fp8_matmul
+    _refused(INVALID, "workspace", f, a, b, d, BF16, n)
+    _refused(INVALID, "workspace", f, a, b, d, BF16, n, None, ws.ctypes.data, nbytes - 4)
+    _refused(ALIGN, "d_workspace", f, a, b, d, BF16, n, None, ws.ctypes.data + 4, nbytes)
+    _refused(INVALID, "overlap", f, a, b, d, BF16, n, None, a.data, nbytes)
 
 
 def test_norm_refuses():

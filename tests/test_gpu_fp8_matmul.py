@@ -56,7 +56,9 @@ def _exact(a, b, c=None):
 
 SIZES = [(1, 1, 1), (1, 16, 128), (2, 3, 5), (1, 300, 1000), (7, 129, 127), (13, 257, 384), (16, 1024, 2048), (17, 64, 129), (31, 500, 640), (33, 128, 256),
          (64, 512, 1111), (65, 70, 512), (100, 1000, 100), (128, 128, 128), (129, 255, 513), (200, 300, 4096), (256, 256, 256), (257, 511, 1030),
-         (300, 40, 3000), (512, 768, 640), (1000, 1001, 130), (600, 1300, 96)]
+         (300, 40, 3000), (512, 768, 640), (1000, 1001, 130), (600, 1300, 96),
+         # each kernel: k shared out (with an end inside a block and inside a group of four), each size of tile with ends on every side
+         (40, 200, 16384), (33, 129, 12345), (100, 64, 7000), (16, 8192, 8000), (260, 4100, 700), (700, 6000, 900), (2050, 2047, 520), (1001, 8190, 250), (3900, 4099, 1100)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
