@@ -288,7 +288,7 @@ extern "C" zi_status zi_rms_norm(const zi_rms_norm_args* args, const zi_fp8_matr
 extern "C" size_t zi_rms_norm_workspace_bytes(int64_t rows, int64_t cols)
 {
     if (rows <= 0 || cols <= 0 || cols > ZI_RMS_NORM_MAX_COLS) return 0;
-    return zi::rms_norm_partials(rows, cols) * (size_t)cols * sizeof(float);
+    return rows > kMostRows ? 0 : zi::rms_norm_workspace_floats(rows, cols) * sizeof(float);
 }
 
 extern "C" zi_status zi_rms_norm_backward(const zi_rms_norm_backward_args* args, void* d_workspace, size_t workspace_bytes,
@@ -311,7 +311,7 @@ extern "C" zi_status zi_rms_norm_backward(const zi_rms_norm_backward_args* args,
         if (zi_status st = check_rows(r.at, a.rows, a.cols, r.ld, r.name)) return st;
     if (!aligned(a.gamma, 2)) return fail(ZI_ERR_ALIGNMENT, "gamma must be 2-byte aligned");
     if (!aligned(a.rstd, 4)) return fail(ZI_ERR_ALIGNMENT, "rstd must be 4-byte aligned");
-    const size_t wanted = a.dgamma ? zi_rms_norm_workspace_bytes(a.rows, a.cols) : 0;
+    const size_t wanted = a.dgamma || zi::rms_norm_needs_means(a.cols) ? zi_rms_norm_workspace_bytes(a.rows, a.cols) : 0;
     if (wanted > 0) {
         if (!d_workspace || workspace_bytes < wanted)
             return fail(ZI_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", d_workspace ? workspace_bytes : (size_t)0, wanted);

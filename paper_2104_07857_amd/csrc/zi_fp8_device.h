@@ -49,6 +49,8 @@ struct Octet {
             }
         }
     }
+    // STREAM: past the caches, for what the kernels that follow do not read at once.
+    template <bool STREAM = false>
     __device__ __forceinline__ void store(void* base, int64_t at, int valid) const
     {
         char* p = static_cast<char*>(base) + at * kBytes;
@@ -58,7 +60,8 @@ struct Octet {
                 vec v;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = w[4 * i + j];
-                reinterpret_cast<vec*>(p)[i] = v;
+                if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<vec*>(p) + i);
+                else reinterpret_cast<vec*>(p)[i] = v;
             }
             return;
         }

@@ -32,8 +32,9 @@ struct RmsNormArgs {
 };
 hipError_t launch_rms_norm(const RmsNormArgs& a, hipStream_t s);
 
-size_t rms_norm_partials(int64_t rows, int64_t cols);     // rows of cols floats that the backward pass leaves
-hipError_t launch_rms_norm_backward(const zi_rms_norm_backward_args& a, float* partials, hipStream_t s);
+size_t rms_norm_workspace_floats(int64_t rows, int64_t cols);     // of the backward pass
+bool rms_norm_needs_means(int64_t cols);                          // it needs them without dgamma too
+hipError_t launch_rms_norm_backward(const zi_rms_norm_backward_args& a, float* workspace, hipStream_t s);
 
 struct MatmulArgs {
     const uint8_t* a;

@@ -142,7 +142,7 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = h[v].get(j) + r.get(j);
                 h[v].set(f);
-                if (a.sum && in[v] > 0) h[v].store(a.sum, row * a.sum_ld + col, in[v]);
+                if (a.sum && in[v] > 0) h[v].template store<true>(a.sum, row * a.sum_ld + col, in[v]);
             }
         }
 #pragma unroll
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
                 if (a.y && in[v] > 0) {
                     Octet<DT> w;
                     w.set(y);
-                    w.store(a.y, row * a.y_ld + col, in[v]);
+                    w.template store<true>(a.y, row * a.y_ld + col, in[v]);
                 }
                 if (k.y8) {
                     const uint32_t byte = scale_byte(max_16(most));
@@ -190,87 +190,135 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
 
 // ---- its backward pass ----------------------------------------------------------------------------------------
 
-// A workgroup goes over rows a grid apart and keeps its columns' share of dgamma in registers; the shares of all
-// workgroups are added by a second kernel in their order.  Rows of up to 32768 columns stay in registers between the
-// sum over the row and what needs it; longer ones are read again.
+// What a thread has of a row: V octets T threads apart, from column `first` on.
 template <int DT, int T, int V>
-__global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_backward_args a, float* partials)
-{
-    constexpr bool kKeep = V < 8;
-    __shared__ float s_sum[T / 64];
-    float share[V][8];
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) share[v][j] = 0.0f;
-    const auto column = [](int v) { return (int64_t)(v * T + threadIdx.x) * 8; };
-    const auto valid = [&](int v) { const int64_t left = a.cols - column(v); return (int)(left < 8 ? left : 8); };
-
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const float rstd = a.rstd[row];
-        Octet<DT> dy[kKeep ? V : 1], h[kKeep ? V : 1], gamma[kKeep ? V : 1];
-        float dot = 0.0f;
+struct BackwardRow {
+    Octet<DT> dy[V], h[V], add[V];
+    float rstd;
+    static __device__ __forceinline__ int64_t column(int64_t first, int v) { return first + (int64_t)(v * T + threadIdx.x) * 8; }
+    static __device__ __forceinline__ int valid(const zi_rms_norm_backward_args& a, int64_t first, int v)
+    {
+        const int64_t left = a.cols - column(first, v);
+        return (int)(left < 8 ? left : 8);
+    }
+    __device__ __forceinline__ void load(const zi_rms_norm_backward_args& a, int64_t row, int64_t first)
+    {
+        rstd = a.rstd[row];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int i = kKeep ? v : 0, in = valid(v);
-            dy[i].load(a.dy, row * a.dy_ld + column(v), in);
-            h[i].load(a.h, row * a.h_ld + column(v), in);
-            gamma[i].load(a.gamma, column(v), in);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) dot = __builtin_fmaf(dy[i].get(j) * gamma[i].get(j), h[i].get(j) * rstd, dot);
+            dy[v].load(a.dy, row * a.dy_ld + column(first, v), valid(a, first, v));
+            h[v].load(a.h, row * a.h_ld + column(first, v), valid(a, first, v));
+            if (a.dsum) add[v].load(a.dsum, row * a.dsum_ld + column(first, v), valid(a, first, v));
         }
-        dot = sum_of_group<T>(dot, s_sum) / (float)a.cols;
+    }
+    __device__ __forceinline__ float dot(const Octet<DT> (&gamma)[V]) const
+    {
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(dy[v].get(j) * gamma[v].get(j), h[v].get(j) * rstd, sum);
+        return sum;
+    }
+    // dx of the row, whose mean of u * n this is, and its share of dgamma
+    __device__ __forceinline__ void finish(const zi_rms_norm_backward_args& a, int64_t row, int64_t first, float mean, const Octet<DT> (&gamma)[V],
+                                           float (&share)[V][8]) const
+    {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int i = kKeep ? v : 0, in = valid(v);
+            const int in = valid(a, first, v);
             if (in <= 0) continue;
-            if constexpr (!kKeep) {
-                dy[0].load(a.dy, row * a.dy_ld + column(v), in);
-                h[0].load(a.h, row * a.h_ld + column(v), in);
-                gamma[0].load(a.gamma, column(v), in);
-            }
-            Octet<DT> add;
-            if (a.dsum) add.load(a.dsum, row * a.dsum_ld + column(v), in);
             float dx[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float n = h[i].get(j) * rstd;
-                dx[j] = rstd * (dy[i].get(j) * gamma[i].get(j) - n * dot);
-                if (a.dsum) dx[j] += add.get(j);
-                share[v][j] = __builtin_fmaf(dy[i].get(j), n, share[v][j]);
+                const float n = h[v].get(j) * rstd;
+                dx[j] = rstd * (dy[v].get(j) * gamma[v].get(j) - n * mean);
+                if (a.dsum) dx[j] += add[v].get(j);
+                share[v][j] = __builtin_fmaf(dy[v].get(j), n, share[v][j]);
             }
             if (a.dx) {
                 Octet<DT> w;
                 w.set(dx);
-                w.store(a.dx, row * a.dx_ld + column(v), in);
+                w.template store<true>(a.dx, row * a.dx_ld + column(first, v), in);
             }
         }
-        if constexpr (T > 64) __syncthreads();                  // s_sum is written again
+    }
+};
+
+// A workgroup goes over rows a grid apart and keeps its columns' share of dgamma in registers; the shares of all
+// workgroups are added by a second kernel in their order.  The next row's loads go out before this row's sum is known (16384 x 4096
+// with dsum 123 -> 97 us).  MEANS: rows of more than 16384 columns do not fit one workgroup's registers; they are cut, and means of whole rows come from a
+// kernel in front (rms_norm_means_kernel), so that dy and h are read twice.
+template <int DT, int T, int V, bool MEANS>
+__global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_backward_args a, float* partials, const float* means, uint32_t cuts)
+{
+    using Row = BackwardRow<DT, T, V>;
+    __shared__ float s_sum[2][T / 64];
+    const uint32_t group = MEANS ? blockIdx.x / cuts : blockIdx.x, groups = MEANS ? gridDim.x / cuts : gridDim.x;
+    const int64_t first = MEANS ? (int64_t)(blockIdx.x % cuts) * (T * V * 8) : 0;
+    float share[V][8] = {};
+    Octet<DT> gamma[V];
+    Row now, next;
+    now.load(a, group, first);
+#pragma unroll
+    for (int v = 0; v < V; ++v) gamma[v].load(a.gamma, Row::column(first, v), Row::valid(a, first, v));
+    int turn = 0;
+    for (int64_t row = group; row < a.rows; row += groups, turn ^= 1) {
+        if (row + groups < a.rows) next.load(a, row + groups, first);
+        float mean;
+        if constexpr (MEANS) mean = means[row];
+        else mean = sum_of_group<T>(now.dot(gamma), s_sum[turn]) / (float)a.cols;
+        now.finish(a, row, first, mean, gamma, share);
+        now = next;
     }
     if (!a.dgamma) return;
-    float* mine = partials + (int64_t)blockIdx.x * a.cols;
+    float* mine = partials + (int64_t)group * a.cols;
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j < valid(v)) mine[column(v) + j] = share[v][j];
+            if (j < Row::valid(a, first, v)) mine[Row::column(first, v) + j] = share[v][j];
 }
 
-// dgamma of 64 columns: 16 wavefronts take every sixteenth share each.
+// The mean of u * n of each row of more than 16384 columns.
+template <int DT>
+__global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_backward_args a, float* means)
+{
+    using Row = BackwardRow<DT, 1024, 2>;
+    __shared__ float s_sum[16];
+    zi_rms_norm_backward_args b = a;
+    b.dsum = nullptr;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        float sum = 0.0f;
+        for (int64_t first = 0; first < a.cols; first += 1024 * 16) {
+            Row r;
+            Octet<DT> gamma[2];
+            r.load(b, row, first);
+#pragma unroll
+            for (int v = 0; v < 2; ++v) gamma[v].load(a.gamma, Row::column(first, v), Row::valid(a, first, v));
+            sum += r.dot(gamma);
+        }
+        sum = sum_of_group<1024>(sum, s_sum);
+        if (threadIdx.x == 0) means[row] = sum / (float)a.cols;
+        __syncthreads();                                        // s_sum is written again
+    }
+}
+
+// dgamma of 16 columns: 64 rows of threads take every 64th share each, and are added in a fixed order.
 template <int DT>
 __global__ __launch_bounds__(1024) void rms_norm_dgamma_kernel(const float* partials, int count, int64_t cols, void* dgamma, int accumulate)
 {
-    __shared__ float s_sum[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ float s_sum[64][16];
+    const int in = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const int64_t col = (int64_t)blockIdx.x * 16 + in;
     float sum = 0.0f;
     if (col < cols)
-        for (int i = wave; i < count; i += 16) sum += partials[(int64_t)i * cols + col];
-    s_sum[wave][lane] = sum;
+        for (int i = part; i < count; i += 64) sum += partials[(int64_t)i * cols + col];
+    s_sum[part][in] = sum;
     __syncthreads();
-    if (wave != 0 || col >= cols) return;
+    if (part != 0 || col >= cols) return;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) sum += s_sum[i][lane];
+    for (int i = 1; i < 64; ++i) sum += s_sum[i][in];
     if constexpr (DT == ZI_FP32) {
         float* p = static_cast<float*>(dgamma) + col;
         *p = accumulate ? *p + sum : sum;
@@ -282,20 +330,23 @@ __global__ __launch_bounds__(1024) void rms_norm_dgamma_kernel(const float* part
     }
 }
 
-// Calls f(type, threads, octets) with the shape that holds a row: 64 threads up to 512 columns, 256 up to 8192, 1024 up to 65536.
+// Calls f with the threads and octets a thread that hold a row of up to 16384 columns: two octets each where that makes at least a wavefront.
+// 16384 x 8192 with everything, us: 256 threads with four octets 217, 512 with two 206, 1024 with one 250.
 template <int DT, typename F>
 static void with_row_shape(int64_t cols, const F& f)
 {
     if (cols <= 64 * 8) f.template operator()<DT, 64, 1>();
-    else if (cols <= 256 * 8) f.template operator()<DT, 256, 1>();
+    else if (cols <= 64 * 16) f.template operator()<DT, 64, 2>();
+    else if (cols <= 128 * 16) f.template operator()<DT, 128, 2>();
     else if (cols <= 256 * 16) f.template operator()<DT, 256, 2>();
-    else if (cols <= 256 * 32) f.template operator()<DT, 256, 4>();
-    else if (cols <= 1024 * 16) f.template operator()<DT, 1024, 2>();
-    else if (cols <= 1024 * 32) f.template operator()<DT, 1024, 4>();
-    else f.template operator()<DT, 1024, 8>();
+    else if (cols <= 512 * 16) f.template operator()<DT, 512, 2>();
+    else f.template operator()<DT, 1024, 2>();
 }
 
 namespace {
+constexpr int64_t kMostWhole = 1024 * 16;       // columns of a row that one workgroup of the backward pass has in registers
+constexpr int kCutThreads = 256, kCutCols = kCutThreads * 16;
+
 struct LaunchNorm {
     const RmsNormArgs& a;
     hipStream_t s;
@@ -315,35 +366,69 @@ struct LaunchBackward {
     template <int DT, int T, int V>
     void operator()() const
     {
-        hipLaunchKernelGGL((rms_norm_backward_kernel<DT, T, V>), dim3(groups), dim3(T), 0, s, a, partials);
+        hipLaunchKernelGGL((rms_norm_backward_kernel<DT, T, V, false>), dim3(groups), dim3(T), 0, s, a, partials, (const float*)nullptr, 1u);
+    }
+    template <int DT>
+    void cut() const
+    {
+        float* means = partials + (int64_t)groups * a.cols;
+        const unsigned cuts = (unsigned)((a.cols + kCutCols - 1) / kCutCols);
+        hipLaunchKernelGGL(rms_norm_means_kernel<DT>, dim3((unsigned)(a.rows < 4096 ? a.rows : 4096)), dim3(1024), 0, s, a, means);
+        hipLaunchKernelGGL((rms_norm_backward_kernel<DT, kCutThreads, 2, true>), dim3(groups * cuts), dim3(kCutThreads), 0, s, a, partials, (const float*)means,
+                           cuts);
+    }
+    template <int DT>
+    void of() const
+    {
+        if (a.cols > kMostWhole) cut<DT>();
+        else with_row_shape<DT>(a.cols, *this);
     }
 };
+template <int DT>
+void launch_norm_of(const RmsNormArgs& a, hipStream_t s)
+{
+    const LaunchNorm f{a, s};
+    if (a.a.cols <= kMostWhole) with_row_shape<DT>(a.a.cols, f);
+    else if (a.a.cols <= 2 * kMostWhole) f.template operator()<DT, 1024, 4>();
+    else f.template operator()<DT, 1024, 8>();
+}
 }  // namespace
 
 hipError_t launch_rms_norm(const RmsNormArgs& a, hipStream_t s)
 {
-    if (a.a.dtype == ZI_BF16) with_row_shape<ZI_BF16>(a.a.cols, LaunchNorm{a, s});
-    else with_row_shape<ZI_FP16>(a.a.cols, LaunchNorm{a, s});
+    if (a.a.dtype == ZI_BF16) launch_norm_of<ZI_BF16>(a, s);
+    else launch_norm_of<ZI_FP16>(a, s);
     return hipGetLastError();
 }
 
-size_t rms_norm_partials(int64_t rows, int64_t cols)
+// Workgroups that go over the rows of the backward pass: few, as each has a row and the next under way.  us with
+// 256 / 512 / 1024 / 1536: 16384 x 4096 97 / 101 / 113 / 112, 4096 x 2048 24.1 / 20.9 / 24.4 / 29.0, 16384 x 1024 63 / 39 / 30 / 30, 65536 x 512
+// 166 / 98 / 68 / 60.
+static int64_t backward_groups(int64_t rows, int64_t cols)
 {
-    const int64_t most = cols <= 8192 ? 1024 : 512;
-    return (size_t)(rows < most ? rows : most);
+    const int64_t cuts = (cols + kCutCols - 1) / kCutCols;
+    const int64_t most = cols <= 512 ? 1536 : cols <= 1024 ? 1024 : cols <= 2048 ? 512 : cols <= kMostWhole ? 256 : 768 / cuts;
+    return rows < most ? rows : most;
 }
+
+size_t rms_norm_workspace_floats(int64_t rows, int64_t cols)
+{
+    return (size_t)(backward_groups(rows, cols) * cols + (cols > kMostWhole ? rows : 0));
+}
+bool rms_norm_needs_means(int64_t cols) { return cols > kMostWhole; }
 
 hipError_t launch_rms_norm_backward(const zi_rms_norm_backward_args& a, float* partials, hipStream_t s)
 {
-    const unsigned groups = (unsigned)rms_norm_partials(a.rows, a.cols);
+    const unsigned groups = (unsigned)backward_groups(a.rows, a.cols);
     if (groups > 0) {
-        if (a.dtype == ZI_BF16) with_row_shape<ZI_BF16>(a.cols, LaunchBackward{a, partials, groups, s});
-        else with_row_shape<ZI_FP16>(a.cols, LaunchBackward{a, partials, groups, s});
+        const LaunchBackward f{a, partials, groups, s};
+        if (a.dtype == ZI_BF16) f.of<ZI_BF16>();
+        else f.of<ZI_FP16>();
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (!a.dgamma) return hipSuccess;
-    const dim3 grid((unsigned)((a.cols + 63) / 64)), block(1024);
+    const dim3 grid((unsigned)((a.cols + 15) / 16)), block(1024);
     if (a.dgamma_dtype == ZI_BF16)
         hipLaunchKernelGGL(rms_norm_dgamma_kernel<ZI_BF16>, grid, block, 0, s, partials, (int)groups, a.cols, a.dgamma, a.accumulate);
     else if (a.dgamma_dtype == ZI_FP16)
