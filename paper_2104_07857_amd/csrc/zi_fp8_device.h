@@ -98,11 +98,46 @@ struct Octet {
 
 // ---- the scale of a block -------------------------------------------------------------------------------------
 
-// Magnitudes are compared by their bits, which order as they do; an infinity or NaN counts as zero.
-__device__ __forceinline__ uint32_t magnitude(float x)
+// Magnitudes are compared by their bits, which order as they do: one fp32 or two 16-bit elements of a word at a time.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <int DT>
+constexpr uint32_t kInfinity = DT == ZI_FP32 ? 0x7F800000u : DT == ZI_BF16 ? 0x7F80u : 0x7C00u;
+
+// FINITE: an infinity or NaN counts as zero.
+template <int DT, bool FINITE>
+__device__ __forceinline__ uint32_t magnitudes(uint32_t w)
 {
-    const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
-    return b < 0x7F800000u ? b : 0u;
+    if constexpr (DT == ZI_FP32) {
+        w &= 0x7FFFFFFFu;
+        return FINITE && w >= kInfinity<DT> ? 0u : w;
+    } else {
+        w &= 0x7FFF7FFFu;
+        if constexpr (FINITE) {
+            if ((w & 0xFFFFu) >= kInfinity<DT>) w &= 0xFFFF0000u;
+            if (w >> 16 >= kInfinity<DT>) w &= 0xFFFFu;
+        }
+        return w;
+    }
+}
+__device__ __forceinline__ uint32_t max_of(uint32_t a, uint32_t b) { return a > b ? a : b; }
+template <int DT>
+__device__ __forceinline__ uint32_t max_of_words(uint32_t a, uint32_t b)
+{
+    if constexpr (DT == ZI_FP32) return max_of(a, b);
+    else return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+// The larger element of a word, and its fp32 bits.
+template <int DT>
+__device__ __forceinline__ uint32_t larger(uint32_t w)
+{
+    return DT == ZI_FP32 ? w : max_of(w & 0xFFFFu, w >> 16);
+}
+template <int DT>
+__device__ __forceinline__ uint32_t as_fp32(uint32_t m)
+{
+    if constexpr (DT == ZI_FP32) return m;
+    else if constexpr (DT == ZI_BF16) return m << 16;
+    else return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)m));
 }
 // The e8m0 byte of the smallest power of two s with `most` <= 448 s; 448 is 1.75 * 2^8.  (The bits of an fp32
 // subnormal have no exponent; its scale is the least there is.)
@@ -111,16 +146,58 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t most)
     const int b = (int)(most >> 23) - 8 + ((most & 0x7FFFFFu) > 0x600000u ? 1 : 0);
     return most == 0 ? 127u : (uint32_t)(b > 0 ? b : 0);
 }
-// 1 / scale: a power of two from 2^-120 to 2^127, so that the product with it is exact but for numbers that round to
-// zero anyway.
-__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte > 0 ? byte << 23 : 1u << 22); }
 
-// Four e4m3 numbers, rounded to nearest even.  None is above 448 but infinities, which become NaN.
-__device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d)
+// Two e4m3 numbers into half of a word: elements divided by the scale, rounded to nearest even.  None is above 448 then
+// but infinities, which become NaN.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+template <int HALF>
+__device__ __forceinline__ i16x2 two_e4m3(i16x2 w, float a, float b, float scale)
 {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-    return (uint32_t)w;
+    return __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, scale, HALF);
+}
+template <int DT, int HALF>
+__device__ __forceinline__ i16x2 two_e4m3(i16x2 w, uint32_t ab, float scale)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    if constexpr (DT == ZI_BF16) return __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, ab), scale, HALF);
+    else return __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(f16x2, ab), scale, HALF);
+}
+__device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d, float scale)
+{
+    return __builtin_bit_cast(uint32_t, two_e4m3<1>(two_e4m3<0>(i16x2{0, 0}, a, b, scale), c, d, scale));
+}
+// Eight of a row, and eight that stand below each other.
+template <int DT>
+__device__ __forceinline__ u32x2 eight_e4m3(const Octet<DT>& x, float scale)
+{
+    u32x2 q;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if constexpr (DT == ZI_FP32)
+            q[i] = four_e4m3(x.get(4 * i), x.get(4 * i + 1), x.get(4 * i + 2), x.get(4 * i + 3), scale);
+        else
+            q[i] = __builtin_bit_cast(uint32_t, two_e4m3<DT, 1>(two_e4m3<DT, 0>(i16x2{0, 0}, x.w[2 * i], scale), x.w[2 * i + 1], scale));
+    }
+    return q;
+}
+template <int DT>
+__device__ __forceinline__ u32x2 eight_e4m3_down(const Octet<DT> (&x)[8], int j, float scale)
+{
+    u32x2 q;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if constexpr (DT == ZI_FP32) {
+            q[i] = four_e4m3(x[4 * i].get(j), x[4 * i + 1].get(j), x[4 * i + 2].get(j), x[4 * i + 3].get(j), scale);
+        } else {
+            const uint32_t halves = j % 2 ? 0x07060302u : 0x05040100u;       // the upper or the lower halves of two words
+            const uint32_t ab = __builtin_amdgcn_perm(x[4 * i + 1].w[j / 2], x[4 * i].w[j / 2], halves);
+            const uint32_t cd = __builtin_amdgcn_perm(x[4 * i + 3].w[j / 2], x[4 * i + 2].w[j / 2], halves);
+            q[i] = __builtin_bit_cast(uint32_t, two_e4m3<DT, 1>(two_e4m3<DT, 0>(i16x2{0, 0}, ab, scale), cd, scale));
+        }
+    }
+    return q;
 }
 
 // ---- over lanes -----------------------------------------------------------------------------------------------
@@ -132,8 +209,6 @@ __device__ __forceinline__ uint32_t dpp(uint32_t x)
 }
 constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirror = 0x140;
 
-__device__ __forceinline__ uint32_t max_of(uint32_t a, uint32_t b) { return a > b ? a : b; }
-
 // Largest over the 16 lanes of a row, in each of them.
 __device__ __forceinline__ uint32_t max_16(uint32_t x)
 {
@@ -142,11 +217,12 @@ __device__ __forceinline__ uint32_t max_16(uint32_t x)
     x = max_of(x, dpp<kDppHalfMirror>(x));
     return max_of(x, dpp<kDppMirror>(x));
 }
-// Largest over the four rows of 16 lanes, in each lane for its place in the row.
+// Largest (of a word's elements each) over the four rows of 16 lanes, in each lane for its place in the row.
+template <int DT>
 __device__ __forceinline__ uint32_t max_of_rows(uint32_t x)
 {
-    x = max_of(x, (uint32_t)__shfl_xor((int)x, 16));
-    return max_of(x, (uint32_t)__shfl_xor((int)x, 32));
+    x = max_of_words<DT>(x, (uint32_t)__shfl_xor((int)x, 16));
+    return max_of_words<DT>(x, (uint32_t)__shfl_xor((int)x, 32));
 }
 __device__ __forceinline__ float sum_64(float x)
 {
