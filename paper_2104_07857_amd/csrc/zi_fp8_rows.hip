@@ -15,7 +15,11 @@ namespace zi {
 // wavefronts.  The transposed numbers pass through LDS, which makes rows of 128 bytes of them.
 constexpr int kTile = kFp8Block;
 
-template <int DT>
+// LARGE: the outputs do not stay in the memory-side cache for whoever reads them next.  Their stores pass it by then, and with a transposed
+// output tiles go along diagonals, since those below each other write to rows of it that are the same few channels'.  us, ordinary / so: 32768 x 8192
+// fp32 in squares, both 316 / 287, 16384 x 8192 bf16 114 / 102, 8191 x 8192 bf16 59.5 / 57.8; but quantisation and product of 4096 x 4096 (x 4096) 70 / 75.
+constexpr int64_t kLargeBytes = (int64_t)96 << 20;
+template <int DT, bool LARGE>
 __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
 {
     __shared__ uint32_t s_col[4][kTile / 8 * Octet<DT>::kWords];
@@ -23,7 +27,13 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
     __shared__ __align__(16) uint8_t s_turned[kTile * kTile];
 
     const int t = threadIdx.x, o = t & 15, g = t >> 4, wave = t >> 6;
-    const int64_t tile_row = blockIdx.x / a.tiles_across, tile_col = blockIdx.x % a.tiles_across;
+    const int64_t tile_col = blockIdx.x % a.tiles_across;
+    int64_t tile_row = blockIdx.x / a.tiles_across;
+    if (LARGE && a.turned) tile_row = (tile_row + tile_col) % (gridDim.x / a.tiles_across);
+    const auto put = [](auto x, auto* at) {
+        if constexpr (LARGE) __builtin_nontemporal_store(x, at);
+        else *at = x;
+    };
     const int64_t row0 = tile_row * kTile + g * 8, col0 = tile_col * kTile + o * 8;
     const int64_t left = a.cols - col0;
     const int in_row = left >= 8 ? 8 : left > 0 ? (int)left : 0;
@@ -73,7 +83,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
         for (int i = 0; i < 8; ++i) {
             const uint32_t byte = a.out_square ? all : scale_byte(as_fp32<DT>(max_16(row_most[i])));
             if (row0 + i >= a.rows || in_row == 0) continue;
-            *reinterpret_cast<u32x2*>(a.out + (row0 + i) * a.out_ld + col0) = eight_e4m3<DT>(x[i], scale_of(byte));
+            put(eight_e4m3<DT>(x[i], scale_of(byte)), reinterpret_cast<u32x2*>(a.out + (row0 + i) * a.out_ld + col0));
             if (!a.out_square && o == 0) a.out_scale[(row0 + i) * a.out_scale_ld + tile_col] = (uint8_t)byte;
         }
         if (a.out_square && t == 0) a.out_scale[tile_row * a.out_scale_ld + tile_col] = (uint8_t)all;
@@ -101,19 +111,24 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
         const int c = i * 32 + (t >> 3), part = t & 7;
         const int64_t col = tile_col * kTile + c, row = tile_row * kTile + part * 16;
         if (col >= a.cols || row >= a.rows) continue;
-        *reinterpret_cast<u32x4*>(a.turned + col * a.turned_ld + row) =
-            *reinterpret_cast<const u32x4*>(s_turned + c * kTile + ((part ^ ((c >> 3) & 7)) << 4));
+        put(*reinterpret_cast<const u32x4*>(s_turned + c * kTile + ((part ^ ((c >> 3) & 7)) << 4)),
+            reinterpret_cast<u32x4*>(a.turned + col * a.turned_ld + row));
     }
 }
 
-hipError_t launch_fp8_quantize(const QuantizeArgs& a, int dtype, hipStream_t s)
+template <int DT>
+static hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t s)
 {
     const int64_t tiles = (int64_t)a.tiles_across * ((a.rows + kTile - 1) / kTile);
+    const bool large = a.rows * a.cols * ((a.out ? 1 : 0) + (a.turned ? 1 : 0)) >= kLargeBytes;
     const dim3 grid((unsigned)tiles), block(256);
-    if (dtype == ZI_BF16) hipLaunchKernelGGL(fp8_quantize_kernel<ZI_BF16>, grid, block, 0, s, a);
-    else if (dtype == ZI_FP16) hipLaunchKernelGGL(fp8_quantize_kernel<ZI_FP16>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(fp8_quantize_kernel<ZI_FP32>, grid, block, 0, s, a);
+    if (large) hipLaunchKernelGGL((fp8_quantize_kernel<DT, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((fp8_quantize_kernel<DT, false>), grid, block, 0, s, a);
     return hipGetLastError();
+}
+hipError_t launch_fp8_quantize(const QuantizeArgs& a, int dtype, hipStream_t s)
+{
+    return dtype == ZI_BF16 ? launch_quantize<ZI_BF16>(a, s) : dtype == ZI_FP16 ? launch_quantize<ZI_FP16>(a, s) : launch_quantize<ZI_FP32>(a, s);
 }
 
 // ---- root-mean-square norm ------------------------------------------------------------------------------------

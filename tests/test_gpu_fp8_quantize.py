@@ -82,6 +82,14 @@ def test_large_offsets():
     _check(x, 1, 1)
 
 
+@pytest.mark.parametrize("form,dtype", [((1, 1), torch.bfloat16), ((128, 128), torch.float32), ((0, 1), torch.float16)])
+def test_outputs_larger_than_the_cache(form, dtype):
+    rows, cols = 9001, 12001 if form[0] == 0 else 6007
+    x = normal((rows, cols), 9, dtype=dtype)
+    x[5, 7] = float("nan")
+    _check(x, *form)
+
+
 def test_another_stream_and_a_graph():
     x = normal((300, 700), 6, dtype=torch.bfloat16)
     torch.cuda.synchronize()
