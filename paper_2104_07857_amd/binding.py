@@ -115,12 +115,13 @@ def _not_taken(*args):
     return None
 
 
-# The calls made once per step, for arguments in their usual form (csrc/zi_python.c): a status, or None for other forms.
+# The calls made once per step or layer, for arguments in their usual form (csrc/zi_python.c): a status, or None for other forms.
 _call_norm = _call_norm_noalloc = _call_step = _not_taken
+_call_quantize = _call_matmul = _call_rms_norm = _call_rms_norm_backward = _not_taken
 
 
 def _bind_calls(L):
-    global _call_norm, _call_norm_noalloc, _call_step
+    global _call_norm, _call_norm_noalloc, _call_step, _call_quantize, _call_matmul, _call_rms_norm, _call_rms_norm_backward
     try:
         from . import _zi_call as c
     except ImportError:                # not built: everything goes through ctypes
@@ -129,6 +130,10 @@ def _bind_calls(L):
     if c.bind(address(L.zi_grad_norm), address(L.zi_grad_norm_noalloc), address(L.zi_adamw_step), zi_tensor(),
               zi_adamw_config()):
         _call_norm, _call_norm_noalloc, _call_step = c.grad_norm, c.grad_norm_noalloc, c.adamw_step
+    if c.bind_fp8(address(L.zi_fp8_quantize), address(L.zi_fp8_matmul), address(L.zi_rms_norm), address(L.zi_rms_norm_backward),
+                  zi_fp8_matrix(), zi_rms_norm_args(), zi_rms_norm_backward_args()):
+        _call_quantize, _call_matmul = c.fp8_quantize, c.fp8_matmul
+        _call_rms_norm, _call_rms_norm_backward = c.rms_norm, c.rms_norm_backward
 
 
 def lib() -> ctypes.CDLL:
@@ -514,6 +519,9 @@ def _bytes(buffer, given: Optional[int]) -> int:
 
 def zi_fp8_quantize(x, dtype: int, rows: int, cols: int, ld: int, out: Optional[zi_fp8_matrix] = None,
                     turned: Optional[zi_fp8_matrix] = None, stream=None) -> int:
+    status = _call_quantize(x, dtype, rows, cols, ld, out, turned, stream)
+    if status is not None:
+        return status if status >= 0 else _check(status)
     return _check(lib().zi_fp8_quantize(_addr(x), int(dtype), int(rows), int(cols), int(ld), _ref(out), _ref(turned),
                                         _stream(stream)))
 
@@ -524,11 +532,17 @@ def zi_fp8_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
 
 def zi_fp8_matmul(a: zi_fp8_matrix, b: zi_fp8_matrix, d, dtype: int, ldd: int, c=None, d_workspace=None,
                   workspace_bytes: Optional[int] = None, stream=None) -> int:
+    status = _call_matmul(a, b, d, dtype, ldd, c, d_workspace, workspace_bytes, stream)
+    if status is not None:
+        return status if status >= 0 else _check(status)
     return _check(lib().zi_fp8_matmul(_ref(a), _ref(b), _addr(d), int(dtype), int(ldd), _addr(c), _addr(d_workspace),
                                       _bytes(d_workspace, workspace_bytes), _stream(stream)))
 
 
 def zi_rms_norm(args: zi_rms_norm_args, y8: Optional[zi_fp8_matrix] = None, stream=None) -> int:
+    status = _call_rms_norm(args, y8, stream)
+    if status is not None:
+        return status if status >= 0 else _check(status)
     return _check(lib().zi_rms_norm(_ref(args), _ref(y8), _stream(stream)))
 
 
@@ -538,5 +552,8 @@ def zi_rms_norm_workspace_bytes(rows: int, cols: int) -> int:
 
 def zi_rms_norm_backward(args: zi_rms_norm_backward_args, d_workspace=None, workspace_bytes: Optional[int] = None,
                          stream=None) -> int:
+    status = _call_rms_norm_backward(args, d_workspace, workspace_bytes, stream)
+    if status is not None:
+        return status if status >= 0 else _check(status)
     return _check(lib().zi_rms_norm_backward(_ref(args), _addr(d_workspace), _bytes(d_workspace, workspace_bytes),
                                              _stream(stream)))

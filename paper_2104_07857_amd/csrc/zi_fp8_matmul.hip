@@ -338,7 +338,7 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
     const int own_row = lane / kChunks, own_chunk = lane % kChunks;
     const int64_t col = n0 + wave_n + own_chunk * 8, left = p.n - col;
     const int valid = left < 8 ? (int)left : 8;
-    const auto turn = [&](auto with_c) {
+    const auto put_sums = [&](auto with_c) {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -359,26 +359,50 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
                     *at = u32x2{Octet<OUT>::pair(x[0], x[1]), Octet<OUT>::pair(x[2], x[3])};
                 }
     };
+    // A whole tile's C and D go in batches without a branch between them; at the ends of the matrix row by row.
+    const bool inside = m0 + kM <= p.m && n0 + kN <= p.n;
+    constexpr int kTurns = kRows / kAtOnce, kBatch = kTurns < 16 ? kTurns : 16;
+    const int64_t at0 = (m0 + wave_m + own_row) * p.d_ld + col;
     if (p.c) {
-#pragma unroll 4
+        if (inside) {
+            for (int turn = 0; turn < kTurns; turn += kBatch) {
+                u32x4_of_2 x[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i)
+                    x[i] = *reinterpret_cast<const u32x4_of_2*>(static_cast<const uint16_t*>(p.c) + at0 + (int64_t)(turn + i) * kAtOnce * p.d_ld);
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) *reinterpret_cast<u32x4*>(chunk(own_row + (turn + i) * kAtOnce, own_chunk)) = x[i];
+            }
+        } else {
+            for (int r = own_row; r < kRows; r += kAtOnce) {
+                const int64_t row = m0 + wave_m + r;
+                Octet<OUT> c;
+                c.load(p.c, row * p.d_ld + col, row < p.m ? valid : 0);
+                *reinterpret_cast<u32x4*>(chunk(r, own_chunk)) = u32x4{c.w[0], c.w[1], c.w[2], c.w[3]};
+            }
+        }
+        put_sums(std::true_type());
+    } else {
+        put_sums(std::false_type());
+    }
+    if (inside) {
+        for (int turn = 0; turn < kTurns; turn += kBatch) {
+            u32x4 x[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) x[i] = *reinterpret_cast<const u32x4*>(chunk(own_row + (turn + i) * kAtOnce, own_chunk));
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                *reinterpret_cast<u32x4_of_2*>(static_cast<uint16_t*>(p.d) + at0 + (int64_t)(turn + i) * kAtOnce * p.d_ld) = x[i];
+        }
+    } else {
         for (int r = own_row; r < kRows; r += kAtOnce) {
             const int64_t row = m0 + wave_m + r;
-            Octet<OUT> c;
-            c.load(p.c, row * p.d_ld + col, row < p.m ? valid : 0);
-            *reinterpret_cast<u32x4*>(chunk(r, own_chunk)) = u32x4{c.w[0], c.w[1], c.w[2], c.w[3]};
-        }
-        turn(std::true_type());
-    } else {
-        turn(std::false_type());
-    }
-#pragma unroll 4
-    for (int r = own_row; r < kRows; r += kAtOnce) {
-        const int64_t row = m0 + wave_m + r;
-        const u32x4 x = *reinterpret_cast<const u32x4*>(chunk(r, own_chunk));
-        Octet<OUT> d;
+            const u32x4 x = *reinterpret_cast<const u32x4*>(chunk(r, own_chunk));
+            Octet<OUT> d;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) d.w[w] = x[w];
-        if (row < p.m && valid > 0) d.store(p.d, row * p.d_ld + col, valid);
+            for (int w = 0; w < 4; ++w) d.w[w] = x[w];
+            if (row < p.m && valid > 0) d.store(p.d, row * p.d_ld + col, valid);
+        }
     }
 }
 

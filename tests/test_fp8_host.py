@@ -197,3 +197,56 @@ def test_ordinary_host_memory_is_an_error_and_no_fault():
     with pytest.raises(zi.ZiError) as e:
         zi.zi_fp8_quantize(_half(4, 100), BF16, 4, 100, 100, _matrix(4, 100))
     assert e.value.status in (zi.ZI_ERR_HIP, INVALID)
+
+
+@pytest.fixture
+def direct():
+    from paper_2104_07857_amd import binding
+    from paper_2104_07857_amd import build as zb
+    if not zb.call_can_be_built():
+        pytest.skip("no Python.h or no gcc: every call goes through ctypes")
+    binding.lib()
+    assert binding._call_matmul is not binding._not_taken, zb.CALL_PATH + " is not built"
+    return binding
+
+
+def test_direct_calls_take_the_usual_forms(direct):
+    """A status for them (these are all refused), None for what the general way has to look at."""
+    a, args = _matrix(4, 100), zi.make_rms_norm(_half(4, 100), _half(1, 100)[0], BF16, 1e-5)
+    back = zi.zi_rms_norm_backward_args()
+    torch = pytest.importorskip("torch")
+    ws = torch.zeros(64, dtype=torch.uint8)
+    for stream in (None, 0):
+        assert direct._call_quantize(None, 3, 4, 100, 100, a, None, stream) == INVALID
+        assert direct._call_matmul(a, None, 16, 0, 4, None, ws, None, stream) == INVALID
+        assert direct._call_rms_norm(args, None, stream) == INVALID
+        assert direct._call_rms_norm_backward(back, None, None, stream) == INVALID
+        assert direct._call_rms_norm_backward(back, ws, 64, stream) == INVALID
+    x = _half(4, 100)
+    assert direct._call_quantize(x, 0, 4, 100, 100, a, None, None) is None             # a numpy array's address
+    assert direct._call_quantize(16, 0.0, 4, 100, 100, a, None, None) is None
+    assert direct._call_matmul(args, a, 16, 0, 4, None, None, None, None) is None      # another structure
+    assert direct._call_matmul(a, args, 16, 0, 4, None, None, None, None) is None
+    assert direct._call_matmul(a, a, 16, 0, 4, None, 16, None, None) is None           # an address without its bytes
+    assert direct._call_rms_norm(a, None, None) is None and direct._call_rms_norm(args, back, None) is None
+    assert direct._call_rms_norm_backward(args, None, None, None) is None
+    assert direct._call_rms_norm(args) is None and direct._call_matmul(a, a) is None
+
+
+def test_both_ways_refuse_alike(direct, monkeypatch):
+    a, args = _matrix(4, 100), zi.make_rms_norm(_half(4, 100), _half(1, 100)[0], BF16, 1e-5)
+    calls = [lambda: zi.zi_fp8_quantize(16, 0, 4, 100, 99, a), lambda: zi.zi_fp8_matmul(a, _matrix(6, 101), 16, 0, 6), lambda: zi.zi_rms_norm(args),
+             lambda: zi.zi_rms_norm_backward(zi.zi_rms_norm_backward_args())]
+
+    def said():
+        out = []
+        for call in calls:
+            with pytest.raises(zi.ZiError) as e:
+                call()
+            out.append((e.value.status, e.value.message))
+        return out
+
+    first = said()
+    for name in ("_call_quantize", "_call_matmul", "_call_rms_norm", "_call_rms_norm_backward"):
+        monkeypatch.setattr(direct, name, direct._not_taken)
+    assert said() == first
