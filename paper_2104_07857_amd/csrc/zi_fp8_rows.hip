@@ -140,28 +140,28 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
     __shared__ float s_sum[T / 64];
     constexpr bool kGammaFirst = V <= 2;        // its loads beside the row's, while there are registers for it: 16384 x 8192 168 -> 159 us
     const zi_rms_norm_args& a = k.a;
+    const auto column = [](int v) { return (int64_t)(v * T + threadIdx.x) * 8; };
+    const auto valid = [&](int v) { const int64_t left = a.cols - column(v); return (int)(left < 8 ? left : 8); };
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         Octet<DT> h[V], gammas[kGammaFirst ? V : 1];
-        int in[V];
         float sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int64_t col = (int64_t)(v * T + threadIdx.x) * 8;
-            in[v] = (int)(a.cols - col < 8 ? a.cols - col : 8);
-            h[v].load(a.x, row * a.x_ld + col, in[v]);
-            if constexpr (kGammaFirst) gammas[v].load(a.gamma, col, in[v]);
+            const int64_t col = column(v);
+            h[v].load(a.x, row * a.x_ld + col, valid(v));
+            if constexpr (kGammaFirst) gammas[v].load(a.gamma, col, valid(v));
         }
         if (a.residual) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int64_t col = (int64_t)(v * T + threadIdx.x) * 8;
+                const int64_t col = column(v);
                 Octet<DT> r;
-                r.load(a.residual, row * a.residual_ld + col, in[v]);
+                r.load(a.residual, row * a.residual_ld + col, valid(v));
                 float f[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = h[v].get(j) + r.get(j);
                 h[v].set(f);
-                if (a.sum && in[v] > 0) h[v].template store<true>(a.sum, row * a.sum_ld + col, in[v]);
+                if (a.sum && valid(v) > 0) h[v].template store<true>(a.sum, row * a.sum_ld + col, valid(v));
             }
         }
 #pragma unroll
@@ -174,21 +174,21 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
         if (a.y || k.y8) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int64_t col = (int64_t)(v * T + threadIdx.x) * 8;
+                const int64_t col = column(v);
                 Octet<DT>& gamma = gammas[kGammaFirst ? v : 0];
-                if constexpr (!kGammaFirst) gamma.load(a.gamma, col, in[v]);
+                if constexpr (!kGammaFirst) gamma.load(a.gamma, col, valid(v));
                 float y[8];
                 uint32_t most = 0;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     y[j] = h[v].get(j) * rstd * gamma.get(j);
-                    if (j >= in[v]) y[j] = 0.0f;                 // (0 times an infinite rstd would be NaN)
+                    if (j >= valid(v)) y[j] = 0.0f;                 // (0 times an infinite rstd would be NaN)
                     most = max_of(most, magnitudes<ZI_FP32, false>(__float_as_uint(y[j])));
                 }
-                if (a.y && in[v] > 0) {
+                if (a.y && valid(v) > 0) {
                     Octet<DT> w;
                     w.set(y);
-                    w.template store<true>(a.y, row * a.y_ld + col, in[v]);
+                    w.template store<true>(a.y, row * a.y_ld + col, valid(v));
                 }
                 if (k.y8) {
                     if (most >= kInfinity<ZI_FP32>) {
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
                         for (int j = 0; j < 8; ++j) most = max_of(most, magnitudes<ZI_FP32, true>(__float_as_uint(y[j])));
                     }
                     const uint32_t byte = scale_byte(max_16(most));
-                    if (in[v] > 0) {
+                    if (valid(v) > 0) {
                         const float scale = scale_of(byte);
                         *reinterpret_cast<u32x2*>(k.y8 + row * k.y8_ld + col) =
                             u32x2{four_e4m3(y[0], y[1], y[2], y[3], scale), four_e4m3(y[4], y[5], y[6], y[7], scale)};
@@ -230,8 +230,13 @@ struct BackwardRow {
         for (int v = 0; v < V; ++v) {
             dy[v].load(a.dy, row * a.dy_ld + column(first, v), valid(a, first, v));
             h[v].load(a.h, row * a.h_ld + column(first, v), valid(a, first, v));
-            if (a.dsum) add[v].load(a.dsum, row * a.dsum_ld + column(first, v), valid(a, first, v));
         }
+    }
+    __device__ __forceinline__ void load_dsum(const zi_rms_norm_backward_args& a, int64_t row, int64_t first)
+    {
+        if (!a.dsum) return;
+#pragma unroll
+        for (int v = 0; v < V; ++v) add[v].load(a.dsum, row * a.dsum_ld + column(first, v), valid(a, first, v));
     }
     __device__ __forceinline__ float dot(const Octet<DT> (&gamma)[V]) const
     {
@@ -275,6 +280,7 @@ template <int DT, int T, int V, bool MEANS>
 __global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_backward_args a, float* partials, const float* means, uint32_t cuts)
 {
     using Row = BackwardRow<DT, T, V>;
+    constexpr bool kAhead = T < 1024;          // dsum too; 1024 threads have 128 registers each, and no room for it
     __shared__ float s_sum[2][T / 64];
     const uint32_t group = MEANS ? blockIdx.x / cuts : blockIdx.x, groups = MEANS ? gridDim.x / cuts : gridDim.x;
     const int64_t first = MEANS ? (int64_t)(blockIdx.x % cuts) * (T * V * 8) : 0;
@@ -282,11 +288,16 @@ __global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_
     Octet<DT> gamma[V];
     Row now, next;
     now.load(a, group, first);
+    if constexpr (kAhead) now.load_dsum(a, group, first);
 #pragma unroll
     for (int v = 0; v < V; ++v) gamma[v].load(a.gamma, Row::column(first, v), Row::valid(a, first, v));
     int turn = 0;
     for (int64_t row = group; row < a.rows; row += groups, turn ^= 1) {
-        if (row + groups < a.rows) next.load(a, row + groups, first);
+        if constexpr (!kAhead) now.load_dsum(a, row, first);
+        if (row + groups < a.rows) {
+            next.load(a, row + groups, first);
+            if constexpr (kAhead) next.load_dsum(a, row + groups, first);
+        }
         float mean;
         if constexpr (MEANS) mean = means[row];
         else mean = sum_of_group<T>(now.dot(gamma), s_sum[turn]) / (float)a.cols;
@@ -308,14 +319,12 @@ __global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_
 {
     using Row = BackwardRow<DT, 1024, 2>;
     __shared__ float s_sum[16];
-    zi_rms_norm_backward_args b = a;
-    b.dsum = nullptr;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         float sum = 0.0f;
         for (int64_t first = 0; first < a.cols; first += 1024 * 16) {
             Row r;
             Octet<DT> gamma[2];
-            r.load(b, row, first);
+            r.load(a, row, first);
 #pragma unroll
             for (int v = 0; v < 2; ++v) gamma[v].load(a.gamma, Row::column(first, v), Row::valid(a, first, v));
             sum += r.dot(gamma);
