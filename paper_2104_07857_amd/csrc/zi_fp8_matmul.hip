@@ -553,18 +553,30 @@ constexpr TileShape kShape[kShapes] = {{64, 64, 2, 0.25f, 0.40f, 3.5f},
                                        {128, 128, 2, 0.70f, 0.95f, 5.5f},
                                        {256, 256, 1, 1.05f, 1.60f, 10.0f}};
 constexpr int64_t kUnits = 256;                  // compute units
-constexpr float kStream = 6.0e6f, kFewStream = 4.7e6f, kJoinStream = 3.0e6f, kJoin = 3.0f, kFewBesides = 3.0f;      // bytes a us; us
+constexpr float kStream = 6.0e6f, kJoinStream = 3.0e6f, kJoin = 2.4f, kJoinPart = 0.3f;            // bytes a us; us
+constexpr float kFewStream = 7.2e6f, kFewOfA = 0.75f / 16.0f, kFewTurn = 3.5f, kFewBesides = 2.0f;
 
-// The least of these estimates: a kernel for few rows of A, where it reads B at 4.7 TB/s (2.9 us for 1 x 1024 x 1024 and 5.1 for 1 x 4096 x 4096, tiles
-// 5.3 and 8.7; but 13.5 for 1 x 16384 x 4096, tiles 11.9), or tiles, and of the smallest as many parts of k as pay for adding them (13 x 4096 x
-// 16384 in one, two, four, eight parts 35.1, 22.0, 15.3, 16.8).
+// The kernel for few rows of A: how fast B comes, which A's rows share the way with, or the turns that a wavefront takes to its loads where few
+// workgroups share a compute unit.  By the formula / measured: 1 x 4096 x 4096 5.5 / 4.8, 16 x 1024 x 16384 16 / 16.9, 1 x 8192 x 8192 11.3 / 12.7,
+// 13 x 4096 x 16384 17.0 / 18.1, 32 x 8192 x 8192 25.3 / 25.9.
+static float few_rows_estimate(int64_t m, int64_t n, int64_t k)
+{
+    const float stream = (float)n * (float)k * (1.0f + kFewOfA * (float)m) / kFewStream;
+    const int64_t turns = ((k + 32 * kStep - 1) / (32 * kStep)) * ((n + 16 * 512 - 1) / (16 * 512));
+    const float wait = (float)turns * kFewTurn;
+    return (stream > wait ? stream : wait) + kFewBesides;
+}
+
+// The least of these estimates: the kernel for few rows of A (2.3 us for 1 x 1024 x 1024 and 4.8 for 1 x 4096 x 4096, tiles 5.3 and 8.7; but 13.4 for
+// 1 x 16384 x 4096, tiles 11.9), or tiles, and of the smallest as many parts of k as pay for adding them (13 x 4096 x 16384 in one, two, four,
+// eight parts 35.1, 22.0, 15.3, 16.8).
 MatmulPlan plan_fp8_matmul(int64_t m, int64_t n, int64_t k)
 {
     const int64_t steps = (k + kStep - 1) / kStep;
     const float stream = ((float)m + (float)n) * (float)k;
     MatmulPlan best{-1, 1, (uint32_t)((steps + 3) / 4 * 4)};
     float least = INFINITY;
-    if (m <= 32) least = kFewBesides + (m <= 16 ? 1.0f : 1.25f) * stream / kFewStream;
+    if (m <= 32) least = few_rows_estimate(m, n, k);
     for (int i = 0; i < kShapes; ++i) {
         const TileShape& t = kShape[i];
         const int64_t tiles = ((m + t.rows - 1) / t.rows) * ((n + t.cols - 1) / t.cols);
@@ -576,7 +588,7 @@ MatmulPlan plan_fp8_matmul(int64_t m, int64_t n, int64_t k)
             const bool apart = t.together == 2 ? rest <= kUnits : rounds == 0 && rest <= kUnits / 2;
             const float work = (float)rounds * round(t.step_together) + (rest ? round(apart ? t.step : t.step_together) : 0.0f);
             float all = 0.01f * work + (work > stream / kStream ? work : stream / kStream);
-            if (really > 1) all += kJoin + 8.0f * (float)really * (float)m * (float)n / kJoinStream;
+            if (really > 1) all += kJoin + (float)really * kJoinPart + 8.0f * (float)really * (float)m * (float)n / kJoinStream;
             if (all < least) {
                 least = all;
                 best = {i, (uint32_t)really, (uint32_t)each};
