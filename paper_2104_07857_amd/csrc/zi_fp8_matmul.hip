@@ -260,19 +260,26 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
         constexpr int kEnd = kFirst + kEach < kPieces ? kFirst + kEach : kPieces;
         for_each<kEnd - kFirst>([&](auto f) { read_one(number<kFirst + f.value>(), to, step, h); });
     };
+    // A step's loads go out evenly over a step's multiplications, or over half of them where they have to be there at its end: 8192 x 8192 x
+    // 8192 415 us over half, 428 over three quarters; 2048 x 2048 x 2048 in 128 x 128 (4 steps) 13.0 over half, 12.5 over all.
+    const auto fetch_share = [&](auto s, uint32_t step) {
+        constexpr int kSpan = RING == 2 ? kSlots : 2 * kSlots;
+        constexpr int kFirst = s.value < kSpan ? s.value * kLoads / kSpan : kLoads, kEnd = s.value < kSpan ? (s.value + 1) * kLoads / kSpan : kLoads;
+        for_each<kEnd - kFirst>([&](auto l) { fetch_one(number<kFirst + l.value>(), step); });
+    };
     Half first, second;
     const auto go = [&](uint32_t step, auto loads) {
         read_scales(words, step);
         for_each<kSlots>([&](auto s) {
             read_share(s, first, step, 0);
-            constexpr int kFirst = s.value * kLoads / kSlots, kEnd = (s.value + 1) * kLoads / kSlots;
-            if constexpr (decltype(loads)::value) for_each<kEnd - kFirst>([&](auto l) { fetch_one(number<kFirst + l.value>(), step + RING - 1); });
+            if constexpr (decltype(loads)::value) fetch_share(s, step + RING - 1);
             multiply_one(s, second, scale);
             __builtin_amdgcn_sched_barrier(0);
         });
         take_scales(words, step);
         for_each<kSlots>([&](auto s) {
             read_share(s, second, step, 1);
+            if constexpr (decltype(loads)::value) fetch_share(number<kSlots + s.value>(), step + RING - 1);
             multiply_one(s, first, scale);
             __builtin_amdgcn_sched_barrier(0);
         });
