@@ -113,7 +113,7 @@ zi_status zi_rms_norm(const zi_rms_norm_args* args, const zi_fp8_matrix* y8, voi
  * cols in dgamma_dtype (dtype or ZI_FP32), or NULL; with accumulate != 0 it is added to, rounded once.  dx may be NULL,
  * or dy, or dsum in place.  The sum over rows is made in fp32 in a fixed order.  d_workspace: device, 16-byte aligned, at least
  * zi_rms_norm_workspace_bytes(rows, cols) bytes, as in zi_fp8_matmul; may be NULL if dgamma is and
- * cols is at most 16384.  1 <= cols <= 65536.
+ * cols is at most 8192.  1 <= cols <= 65536.
  */
 typedef struct {
     const void* dy;

@@ -384,7 +384,11 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
             for (int r = own_row; r < kRows; r += kAtOnce) {
                 const int64_t row = m0 + wave_m + r;
                 Octet<OUT> c;
-                c.load(p.c, row * p.d_ld + col, row < p.m ? valid : 0);
+                c.clear();
+                if (row < p.m) {
+                    c.template load<Ends::kMoved>(p.c, row * p.d_ld + col, valid, p.n);
+                    c.template settle<Ends::kMoved>(valid, p.n);
+                }
                 *reinterpret_cast<u32x4*>(chunk(r, own_chunk)) = u32x4{c.w[0], c.w[1], c.w[2], c.w[3]};
             }
         }

@@ -36,11 +36,18 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
     };
     const int64_t row0 = tile_row * kTile + g * 8, col0 = tile_col * kTile + o * 8;
     const int64_t left = a.cols - col0;
-    const int in_row = left >= 8 ? 8 : left > 0 ? (int)left : 0;
+    const int in_row = left >= 8 ? 8 : left > 0 ? (int)left : 0, in_row_or_less = left >= 8 ? 8 : (int)left;
 
     Octet<DT> x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i].load(a.x, (row0 + i) * a.ld + col0, row0 + i < a.rows ? in_row : 0);
+    for (int i = 0; i < 8; ++i) {
+        x[i].clear();
+        if (row0 + i < a.rows) x[i].template load<Ends::kMoved>(a.x, (row0 + i) * a.ld + col0, in_row_or_less, a.cols);
+    }
+    if (in_row < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i].template settle<Ends::kMoved>(in_row_or_less, a.cols);
+    }
 
     constexpr int kWords = Octet<DT>::kWords;
     uint32_t row_most[8], col_most[kWords], most;
@@ -134,29 +141,39 @@ hipError_t launch_fp8_quantize(const QuantizeArgs& a, int dtype, hipStream_t s)
 // ---- root-mean-square norm ------------------------------------------------------------------------------------
 
 // T threads have a row, V octets each: octet v * T + t.  16 lanes have a block of 128 columns.
-template <int DT, int T, int V>
+template <int DT, int T, int V, bool RAGGED>
 __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
 {
     __shared__ float s_sum[T / 64];
-    constexpr bool kGammaFirst = V <= 2;        // its loads beside the row's, while there are registers for it: 16384 x 8192 168 -> 159 us
+    constexpr bool kAllFirst = V <= 2;          // all loads in front of what uses them, while there are registers for them
+    constexpr Ends kEnds = !RAGGED ? Ends::kWhole : V <= 4 ? Ends::kMoved : Ends::kApart;      // (eight octets leave no registers for moving)
     const zi_rms_norm_args& a = k.a;
-    const auto column = [](int v) { return (int64_t)(v * T + threadIdx.x) * 8; };
-    const auto valid = [&](int v) { const int64_t left = a.cols - column(v); return (int)(left < 8 ? left : 8); };
+    const int cols = (int)a.cols, own = (int)threadIdx.x * 8;                    // (columns are at most 65536)
+    const auto column = [&](int v) { return own + v * T * 8; };
+    const auto valid = [&](int v) { return cols - column(v) < 8 ? cols - column(v) : 8; };
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        Octet<DT> h[V], gammas[kGammaFirst ? V : 1];
+        Octet<DT> h[V], gammas[kAllFirst ? V : 1];
         float sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int64_t col = column(v);
-            h[v].load(a.x, row * a.x_ld + col, valid(v));
-            if constexpr (kGammaFirst) gammas[v].load(a.gamma, col, valid(v));
+            const int col = column(v);
+            h[v].template load<kEnds>(a.x, row * a.x_ld + col, valid(v), a.cols);
+            if constexpr (kAllFirst) gammas[v].template load<kEnds>(a.gamma, col, valid(v), a.cols);
         }
+        Octet<DT> residual[kAllFirst ? V : 1];
+        if (kAllFirst && a.residual) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) residual[kAllFirst ? v : 0].template load<kEnds>(a.residual, row * a.residual_ld + column(v), valid(v), a.cols);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v].template settle<kEnds>(valid(v), a.cols);
         if (a.residual) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int64_t col = column(v);
-                Octet<DT> r;
-                r.load(a.residual, row * a.residual_ld + col, valid(v));
+                const int col = column(v);
+                Octet<DT>& r = residual[kAllFirst ? v : 0];
+                if constexpr (!kAllFirst) r.template load<kEnds>(a.residual, row * a.residual_ld + col, valid(v), a.cols);
+                r.template settle<kEnds>(valid(v), a.cols);
                 float f[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = h[v].get(j) + r.get(j);
@@ -174,9 +191,10 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
         if (a.y || k.y8) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int64_t col = column(v);
-                Octet<DT>& gamma = gammas[kGammaFirst ? v : 0];
-                if constexpr (!kGammaFirst) gamma.load(a.gamma, col, valid(v));
+                const int col = column(v);
+                Octet<DT>& gamma = gammas[kAllFirst ? v : 0];
+                if constexpr (!kAllFirst) gamma.template load<kEnds>(a.gamma, col, valid(v), a.cols);
+                gamma.template settle<kEnds>(valid(v), a.cols);
                 float y[8];
                 uint32_t most = 0;
 #pragma unroll
@@ -213,30 +231,40 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
 // ---- its backward pass ----------------------------------------------------------------------------------------
 
 // What a thread has of a row: V octets T threads apart, from column `first` on.
-template <int DT, int T, int V>
+template <int DT, int T, int V, bool RAGGED>
 struct BackwardRow {
+    static constexpr Ends kEnds = RAGGED ? Ends::kMoved : Ends::kWhole;
     Octet<DT> dy[V], h[V], add[V];
     float rstd;
-    static __device__ __forceinline__ int64_t column(int64_t first, int v) { return first + (int64_t)(v * T + threadIdx.x) * 8; }
-    static __device__ __forceinline__ int valid(const zi_rms_norm_backward_args& a, int64_t first, int v)
+    static __device__ __forceinline__ int column(int first, int v) { return first + (v * T + (int)threadIdx.x) * 8; }
+    static __device__ __forceinline__ int valid(const zi_rms_norm_backward_args& a, int first, int v)
     {
-        const int64_t left = a.cols - column(first, v);
-        return (int)(left < 8 ? left : 8);
+        const int left = (int)a.cols - column(first, v);
+        return left < 8 ? left : 8;
     }
-    __device__ __forceinline__ void load(const zi_rms_norm_backward_args& a, int64_t row, int64_t first)
+    __device__ __forceinline__ void load(const zi_rms_norm_backward_args& a, int64_t row, int first)
     {
         rstd = a.rstd[row];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            dy[v].load(a.dy, row * a.dy_ld + column(first, v), valid(a, first, v));
-            h[v].load(a.h, row * a.h_ld + column(first, v), valid(a, first, v));
+            dy[v].template load<kEnds>(a.dy, row * a.dy_ld + column(first, v), valid(a, first, v), a.cols);
+            h[v].template load<kEnds>(a.h, row * a.h_ld + column(first, v), valid(a, first, v), a.cols);
         }
     }
-    __device__ __forceinline__ void load_dsum(const zi_rms_norm_backward_args& a, int64_t row, int64_t first)
+    __device__ __forceinline__ void load_dsum(const zi_rms_norm_backward_args& a, int64_t row, int first)
     {
         if (!a.dsum) return;
 #pragma unroll
-        for (int v = 0; v < V; ++v) add[v].load(a.dsum, row * a.dsum_ld + column(first, v), valid(a, first, v));
+        for (int v = 0; v < V; ++v) add[v].template load<kEnds>(a.dsum, row * a.dsum_ld + column(first, v), valid(a, first, v), a.cols);
+    }
+    __device__ __forceinline__ void settle(const zi_rms_norm_backward_args& a, int first)
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            dy[v].template settle<kEnds>(valid(a, first, v), a.cols);
+            h[v].template settle<kEnds>(valid(a, first, v), a.cols);
+            if (a.dsum) add[v].template settle<kEnds>(valid(a, first, v), a.cols);
+        }
     }
     __device__ __forceinline__ float dot(const Octet<DT> (&gamma)[V]) const
     {
@@ -248,7 +276,7 @@ struct BackwardRow {
         return sum;
     }
     // dx of the row, whose mean of u * n this is, and its share of dgamma
-    __device__ __forceinline__ void finish(const zi_rms_norm_backward_args& a, int64_t row, int64_t first, float mean, const Octet<DT> (&gamma)[V],
+    __device__ __forceinline__ void finish(const zi_rms_norm_backward_args& a, int64_t row, int first, float mean, const Octet<DT> (&gamma)[V],
                                            float (&share)[V][8]) const
     {
 #pragma unroll
@@ -274,23 +302,26 @@ struct BackwardRow {
 
 // A workgroup goes over rows a grid apart and keeps its columns' share of dgamma in registers; the shares of all
 // workgroups are added by a second kernel in their order.  The next row's loads go out before this row's sum is known (16384 x 4096
-// with dsum 123 -> 97 us).  MEANS: rows of more than 16384 columns do not fit one workgroup's registers; they are cut, and means of whole rows come from a
-// kernel in front (rms_norm_means_kernel), so that dy and h are read twice.
-template <int DT, int T, int V, bool MEANS>
+// with dsum 123 -> 97 us).  MEANS: rows that do not fit one workgroup's registers (is_cut) are cut, and means of whole rows come from a kernel in
+// front (rms_norm_means_kernel), so that dy and h are read twice.
+template <int DT, int T, int V, bool MEANS, bool RAGGED>
 __global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_backward_args a, float* partials, const float* means, uint32_t cuts)
 {
-    using Row = BackwardRow<DT, T, V>;
+    using Row = BackwardRow<DT, T, V, RAGGED>;
     constexpr bool kAhead = T < 1024;          // dsum too; 1024 threads have 128 registers each, and no room for it
     __shared__ float s_sum[2][T / 64];
     const uint32_t group = MEANS ? blockIdx.x / cuts : blockIdx.x, groups = MEANS ? gridDim.x / cuts : gridDim.x;
-    const int64_t first = MEANS ? (int64_t)(blockIdx.x % cuts) * (T * V * 8) : 0;
+    const int first = MEANS ? (int)(blockIdx.x % cuts) * (T * V * 8) : 0;
     float share[V][8] = {};
     Octet<DT> gamma[V];
     Row now, next;
     now.load(a, group, first);
     if constexpr (kAhead) now.load_dsum(a, group, first);
 #pragma unroll
-    for (int v = 0; v < V; ++v) gamma[v].load(a.gamma, Row::column(first, v), Row::valid(a, first, v));
+    for (int v = 0; v < V; ++v) {
+        gamma[v].template load<Row::kEnds>(a.gamma, Row::column(first, v), Row::valid(a, first, v), a.cols);
+        gamma[v].template settle<Row::kEnds>(Row::valid(a, first, v), a.cols);
+    }
     int turn = 0;
     for (int64_t row = group; row < a.rows; row += groups, turn ^= 1) {
         if constexpr (!kAhead) now.load_dsum(a, row, first);
@@ -298,6 +329,7 @@ __global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_
             next.load(a, row + groups, first);
             if constexpr (kAhead) next.load_dsum(a, row + groups, first);
         }
+        now.settle(a, first);
         float mean;
         if constexpr (MEANS) mean = means[row];
         else mean = sum_of_group<T>(now.dot(gamma), s_sum[turn]) / (float)a.cols;
@@ -313,20 +345,25 @@ __global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_
             if (j < Row::valid(a, first, v)) mine[Row::column(first, v) + j] = share[v][j];
 }
 
-// The mean of u * n of each row of more than 16384 columns.
-template <int DT>
+// The mean of u * n of each row.
+template <int DT, bool RAGGED>
 __global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_backward_args a, float* means)
 {
-    using Row = BackwardRow<DT, 1024, 2>;
+    using Row = BackwardRow<DT, 1024, 2, RAGGED>;
     __shared__ float s_sum[16];
+    zi_rms_norm_backward_args b = a;             // without dsum, which is not loaded
+    b.dsum = nullptr;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         float sum = 0.0f;
-        for (int64_t first = 0; first < a.cols; first += 1024 * 16) {
+        for (int first = 0; first < (int)a.cols; first += 1024 * 16) {
             Row r;
             Octet<DT> gamma[2];
             r.load(a, row, first);
 #pragma unroll
-            for (int v = 0; v < 2; ++v) gamma[v].load(a.gamma, Row::column(first, v), Row::valid(a, first, v));
+            for (int v = 0; v < 2; ++v) gamma[v].template load<Row::kEnds>(a.gamma, Row::column(first, v), Row::valid(a, first, v), a.cols);
+            r.settle(b, first);
+#pragma unroll
+            for (int v = 0; v < 2; ++v) gamma[v].template settle<Row::kEnds>(Row::valid(a, first, v), a.cols);
             sum += r.dot(gamma);
         }
         sum = sum_of_group<1024>(sum, s_sum);
@@ -335,21 +372,21 @@ __global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_
     }
 }
 
-// dgamma of 16 columns: 64 rows of threads take every 64th share each, and are added in a fixed order.
-template <int DT>
-__global__ __launch_bounds__(1024) void rms_norm_dgamma_kernel(const float* partials, int count, int64_t cols, void* dgamma, int accumulate)
+// dgamma of 16 columns: P rows of threads take every Pth share each, and are added in a fixed order.
+template <int DT, int P>
+__global__ __launch_bounds__(16 * P) void rms_norm_dgamma_kernel(const float* partials, int count, int64_t cols, void* dgamma, int accumulate)
 {
-    __shared__ float s_sum[64][16];
+    __shared__ float s_sum[P][16];
     const int in = threadIdx.x & 15, part = threadIdx.x >> 4;
     const int64_t col = (int64_t)blockIdx.x * 16 + in;
     float sum = 0.0f;
     if (col < cols)
-        for (int i = part; i < count; i += 64) sum += partials[(int64_t)i * cols + col];
+        for (int i = part; i < count; i += P) sum += partials[(int64_t)i * cols + col];
     s_sum[part][in] = sum;
     __syncthreads();
     if (part != 0 || col >= cols) return;
 #pragma unroll
-    for (int i = 1; i < 64; ++i) sum += s_sum[i][in];
+    for (int i = 1; i < P; ++i) sum += s_sum[i][in];
     if constexpr (DT == ZI_FP32) {
         float* p = static_cast<float*>(dgamma) + col;
         *p = accumulate ? *p + sum : sum;
@@ -375,7 +412,9 @@ static void with_row_shape(int64_t cols, const F& f)
 }
 
 namespace {
-constexpr int64_t kMostWhole = 1024 * 16;       // columns of a row that one workgroup of the backward pass has in registers
+// Whether one workgroup of the backward pass has a row in registers: up to 16384 columns, or 8192 where they are not whole octets, which takes more
+// registers than 1024 threads have.
+bool is_cut(int64_t cols) { return cols > (cols % 8 ? 512 * 16 : 1024 * 16); }
 constexpr int kCutThreads = 256, kCutCols = kCutThreads * 16;
 
 struct LaunchNorm {
@@ -386,7 +425,8 @@ struct LaunchNorm {
     {
         const int64_t most = (int64_t)1 << 20;
         const dim3 grid((unsigned)(a.a.rows < most ? a.a.rows : most)), block(T);
-        hipLaunchKernelGGL((rms_norm_kernel<DT, T, V>), grid, block, 0, s, a);
+        if (a.a.cols % 8) hipLaunchKernelGGL((rms_norm_kernel<DT, T, V, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((rms_norm_kernel<DT, T, V, false>), grid, block, 0, s, a);
     }
 };
 struct LaunchBackward {
@@ -397,21 +437,32 @@ struct LaunchBackward {
     template <int DT, int T, int V>
     void operator()() const
     {
-        hipLaunchKernelGGL((rms_norm_backward_kernel<DT, T, V, false>), dim3(groups), dim3(T), 0, s, a, partials, (const float*)nullptr, 1u);
+        launch<DT, T, V, false>(groups, nullptr, 1);
+    }
+    template <int DT, int T, int V, bool MEANS>
+    void launch(unsigned grid, const float* means, unsigned cuts) const
+    {
+        if constexpr (T < 1024)
+            if (a.cols % 8) {
+                hipLaunchKernelGGL((rms_norm_backward_kernel<DT, T, V, MEANS, true>), dim3(grid), dim3(T), 0, s, a, partials, means, cuts);
+                return;
+            }
+        hipLaunchKernelGGL((rms_norm_backward_kernel<DT, T, V, MEANS, false>), dim3(grid), dim3(T), 0, s, a, partials, means, cuts);
     }
     template <int DT>
     void cut() const
     {
         float* means = partials + (int64_t)groups * a.cols;
         const unsigned cuts = (unsigned)((a.cols + kCutCols - 1) / kCutCols);
-        hipLaunchKernelGGL(rms_norm_means_kernel<DT>, dim3((unsigned)(a.rows < 4096 ? a.rows : 4096)), dim3(1024), 0, s, a, means);
-        hipLaunchKernelGGL((rms_norm_backward_kernel<DT, kCutThreads, 2, true>), dim3(groups * cuts), dim3(kCutThreads), 0, s, a, partials, (const float*)means,
-                           cuts);
+        const dim3 grid((unsigned)(a.rows < 4096 ? a.rows : 4096)), block(1024);
+        if (a.cols % 8) hipLaunchKernelGGL((rms_norm_means_kernel<DT, true>), grid, block, 0, s, a, means);
+        else hipLaunchKernelGGL((rms_norm_means_kernel<DT, false>), grid, block, 0, s, a, means);
+        launch<DT, kCutThreads, 2, true>(groups * cuts, means, cuts);
     }
     template <int DT>
     void of() const
     {
-        if (a.cols > kMostWhole) cut<DT>();
+        if (is_cut(a.cols)) cut<DT>();
         else with_row_shape<DT>(a.cols, *this);
     }
 };
@@ -419,8 +470,8 @@ template <int DT>
 void launch_norm_of(const RmsNormArgs& a, hipStream_t s)
 {
     const LaunchNorm f{a, s};
-    if (a.a.cols <= kMostWhole) with_row_shape<DT>(a.a.cols, f);
-    else if (a.a.cols <= 2 * kMostWhole) f.template operator()<DT, 1024, 4>();
+    if (a.a.cols <= 1024 * 16) with_row_shape<DT>(a.a.cols, f);
+    else if (a.a.cols <= 1024 * 32) f.template operator()<DT, 1024, 4>();
     else f.template operator()<DT, 1024, 8>();
 }
 }  // namespace
@@ -438,15 +489,23 @@ hipError_t launch_rms_norm(const RmsNormArgs& a, hipStream_t s)
 static int64_t backward_groups(int64_t rows, int64_t cols)
 {
     const int64_t cuts = (cols + kCutCols - 1) / kCutCols;
-    const int64_t most = cols <= 512 ? 1536 : cols <= 1024 ? 1024 : cols <= 2048 ? 512 : cols <= kMostWhole ? 256 : 768 / cuts;
+    const int64_t most = cols <= 512 ? 1536 : cols <= 1024 ? 1024 : cols <= 2048 ? 512 : !is_cut(cols) ? 256 : 768 / cuts;
     return rows < most ? rows : most;
+}
+
+template <int DT>
+static void launch_dgamma(const zi_rms_norm_backward_args& a, const float* partials, int groups, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.cols + 15) / 16));
+    if (groups <= 64) hipLaunchKernelGGL((rms_norm_dgamma_kernel<DT, 16>), grid, dim3(256), 0, s, partials, groups, a.cols, a.dgamma, a.accumulate);
+    else hipLaunchKernelGGL((rms_norm_dgamma_kernel<DT, 64>), grid, dim3(1024), 0, s, partials, groups, a.cols, a.dgamma, a.accumulate);
 }
 
 size_t rms_norm_workspace_floats(int64_t rows, int64_t cols)
 {
-    return (size_t)(backward_groups(rows, cols) * cols + (cols > kMostWhole ? rows : 0));
+    return (size_t)(backward_groups(rows, cols) * cols + (is_cut(cols) ? rows : 0));
 }
-bool rms_norm_needs_means(int64_t cols) { return cols > kMostWhole; }
+bool rms_norm_needs_means(int64_t cols) { return is_cut(cols); }
 
 hipError_t launch_rms_norm_backward(const zi_rms_norm_backward_args& a, float* partials, hipStream_t s)
 {
@@ -459,13 +518,9 @@ hipError_t launch_rms_norm_backward(const zi_rms_norm_backward_args& a, float* p
         if (e != hipSuccess) return e;
     }
     if (!a.dgamma) return hipSuccess;
-    const dim3 grid((unsigned)((a.cols + 15) / 16)), block(1024);
-    if (a.dgamma_dtype == ZI_BF16)
-        hipLaunchKernelGGL(rms_norm_dgamma_kernel<ZI_BF16>, grid, block, 0, s, partials, (int)groups, a.cols, a.dgamma, a.accumulate);
-    else if (a.dgamma_dtype == ZI_FP16)
-        hipLaunchKernelGGL(rms_norm_dgamma_kernel<ZI_FP16>, grid, block, 0, s, partials, (int)groups, a.cols, a.dgamma, a.accumulate);
-    else
-        hipLaunchKernelGGL(rms_norm_dgamma_kernel<ZI_FP32>, grid, block, 0, s, partials, (int)groups, a.cols, a.dgamma, a.accumulate);
+    if (a.dgamma_dtype == ZI_BF16) launch_dgamma<ZI_BF16>(a, partials, (int)groups, s);
+    else if (a.dgamma_dtype == ZI_FP16) launch_dgamma<ZI_FP16>(a, partials, (int)groups, s);
+    else launch_dgamma<ZI_FP32>(a, partials, (int)groups, s);
     return hipGetLastError();
 }
 
