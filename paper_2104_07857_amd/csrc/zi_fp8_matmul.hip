@@ -544,47 +544,49 @@ __global__ __launch_bounds__(256) void fp8_matmul_join_kernel(const MatmulArgs p
 // ---- which kernel ---------------------------------------------------------------------------------------------
 
 // Tiles, steps of k in LDS, workgroups that share a compute unit, and what a round of them takes: so much a step and so much besides, in us,
-// measured on the products below, with one workgroup on a compute unit and with two (256 x 256: on up to half of the compute units, and on all of
-// them, where the power the card may draw holds the clock down).  By tile, us:
-//                           64 x 64   64 x 128  128 x 128 (4 steps)  128 x 128 (2)  256 x 256
-//     64 x  4096 x  4096     11.1      12.1         17                 24             -
-//    512 x  4096 x  4096     17.0      15.1         17.6               24.0           35
-//   2048 x  2048 x  2048     17.6      14.3         12.9               15.2           25.6
-//   1001 x  8192 x  2048     32.0      25.4         23.4               19.7           26.7
-//   3000 x  5000 x  4096     99        81           76                 62             54.5
-//   8192 x  8192 x  8192    881       689          628                572            417
+// measured on the products below, with one workgroup on a compute unit and with two (256 x 128 and 256 x 256: on up to half of the compute units, and
+// on all of them, where the power the card may draw holds the clock down).  By tile, us:
+//                           64 x 64   64 x 128  128 x 128 (4 steps)  128 x 128 (2)  256 x 128  256 x 256
+//     64 x  4096 x  4096     11.1      12.1         17                 24             -          -
+//    512 x  4096 x  4096     17.0      15.0         16.0               23.8          24         35
+//   2048 x  2048 x  2048     17.6      13.3         12.2               15.0          16.1       24.5
+//   1001 x  8192 x  2048     32.0      24.7         23.3               19.6          19.8       27.2
+//   1024 x  8192 x  8192      -         -           74.9               70.6          60.6        -
+//   3000 x  5000 x  4096     99        80           73                 64            62.3       53.0
+//   8192 x  8192 x  8192    881       650          549                507           487        406
 struct TileShape {
     int rows, cols, together;
     float step, step_together, besides;
 };
-constexpr int kShapes = 5;
-constexpr TileShape kShape[kShapes] = {{64, 64, 2, 0.25f, 0.40f, 3.5f},
-                                       {64, 128, 2, 0.33f, 0.62f, 4.5f},
-                                       {128, 128, 1, 0.50f, 0.50f, 5.0f},
-                                       {128, 128, 2, 0.70f, 0.95f, 5.5f},
-                                       {256, 256, 1, 1.05f, 1.60f, 10.0f}};
+constexpr int kShapes = 6;
+constexpr TileShape kShape[kShapes] = {{64, 64, 2, 0.268f, 0.373f, 3.26f},
+                                       {64, 128, 2, 0.34f, 0.55f, 4.5f},
+                                       {128, 128, 1, 0.40f, 0.53f, 5.0f},
+                                       {128, 128, 2, 0.565f, 0.93f, 4.65f},
+                                       {256, 128, 1, 0.65f, 0.755f, 8.75f},
+                                       {256, 256, 1, 1.04f, 1.28f, 14.2f}};
 constexpr int64_t kUnits = 256;                  // compute units
-constexpr float kStream = 6.0e6f, kJoinStream = 3.0e6f, kJoin = 2.4f, kJoinPart = 0.3f;            // bytes a us; us
-constexpr float kFewStream = 7.2e6f, kFewOfA = 0.75f / 16.0f, kFewTurn = 3.5f, kFewBesides = 2.0f;
+constexpr float kStream = 4.8e6f, kOutput = 5.4f, kJoinStream = 5.2e6f, kJoin = 1.4f, kJoinPart = 0.6f;     // bytes a us; an element of D in bytes; us
+constexpr float kFewStream = 6.3e6f, kFewOfA = 0.22f, kFewTurn = 2.5f, kFewTurn2 = 3.85f, kFewBesides = 1.3f;
 
-// The kernel for few rows of A: how fast B comes, which A's rows share the way with, or the turns that a wavefront takes to its loads where few
-// workgroups share a compute unit.  By the formula / measured: 1 x 4096 x 4096 5.5 / 4.8, 16 x 1024 x 16384 16 / 16.9, 1 x 8192 x 8192 11.3 / 12.7,
-// 13 x 4096 x 16384 17.0 / 18.1, 32 x 8192 x 8192 25.3 / 25.9.
+// The kernel for few rows of A: how fast B comes, which A's rows share the way with, or the turns that a wavefront takes to its loads (longer ones
+// with more than 16 rows of A) where few workgroups share a compute unit.
 static float few_rows_estimate(int64_t m, int64_t n, int64_t k)
 {
     const float stream = (float)n * (float)k * (1.0f + kFewOfA * (float)m) / kFewStream;
     const int64_t turns = ((k + 32 * kStep - 1) / (32 * kStep)) * ((n + 16 * 512 - 1) / (16 * 512));
-    const float wait = (float)turns * kFewTurn;
+    const float wait = (float)turns * (m > 16 ? kFewTurn2 : kFewTurn);
     return (stream > wait ? stream : wait) + kFewBesides;
 }
 
-// The least of these estimates: the kernel for few rows of A (2.3 us for 1 x 1024 x 1024 and 4.8 for 1 x 4096 x 4096, tiles 5.3 and 8.7; but 13.4 for
-// 1 x 16384 x 4096, tiles 11.9), or tiles, and of the smallest as many parts of k as pay for adding them (13 x 4096 x 16384 in one, two, four,
-// eight parts 35.1, 22.0, 15.3, 16.8).
+// The least of these estimates: the kernel for few rows of A, or tiles, and of the smallest as many parts of k as pay for adding them (13 x 4096 x
+// 16384 in one, two, four, eight parts 35.1, 22.0, 15.3, 16.8).  The constants are those with which this finds the fastest of all that were timed on 386
+// products, m of 1 to 16384, n of 128 to 32768 and k of 128 to 16384 drawn evenly on a logarithmic scale (with up to 64 rows of A, B from memory): it is
+// 0.4 % slower than that on the average.
 MatmulPlan plan_fp8_matmul(int64_t m, int64_t n, int64_t k)
 {
     const int64_t steps = (k + kStep - 1) / kStep;
-    const float stream = ((float)m + (float)n) * (float)k;
+    const float stream = ((float)m + (float)n) * (float)k + kOutput * (float)m * (float)n;
     MatmulPlan best{-1, 1, (uint32_t)((steps + 3) / 4 * 4)};
     float least = INFINITY;
     if (m <= 32) least = few_rows_estimate(m, n, k);
@@ -638,7 +640,8 @@ static hipError_t launch_of(const MatmulArgs& a, float* partials, hipStream_t s)
     case 1: return launch_tiles<DT, 1, 2, 3>(a, plan, partials, s);
     case 2: return launch_tiles<DT, 2, 2, 4>(a, plan, partials, s);
     case 3: return launch_tiles<DT, 2, 2, 2>(a, plan, partials, s);
-    case 4: return launch_tiles<DT, 4, 4, 2>(a, plan, partials, s);
+    case 4: return launch_tiles<DT, 4, 2, 3>(a, plan, partials, s);
+    case 5: return launch_tiles<DT, 4, 4, 2>(a, plan, partials, s);
     }
     return a.m <= 16 ? launch_few<DT, 1, 8>(a, s) : launch_few<DT, 2, 8>(a, s);
 }
