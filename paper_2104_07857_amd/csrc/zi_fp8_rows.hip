@@ -15,9 +15,25 @@ namespace zi {
 // wavefronts.  The transposed numbers pass through LDS, which makes rows of 128 bytes of them.
 constexpr int kTile = kFp8Block;
 
-// LARGE: the outputs do not stay in the memory-side cache for whoever reads them next.  Their stores pass it by then, and with a transposed
-// output tiles go along diagonals, since those below each other write to rows of it that are the same few channels'.  us, ordinary / so: 32768 x 8192
-// fp32 in squares, both 316 / 287, 16384 x 8192 bf16 114 / 102, 8191 x 8192 bf16 59.5 / 57.8; but quantisation and product of 4096 x 4096 (x 4096) 70 / 75.
+// Each XCD has a run of tiles that goes down four rows of tiles before the next column, so that its L2 joins the bytes that neighbours write
+// to a line of scales, and begins at another eighth of its run, so that all of them do not go through the same memory channels at a time.  us, row by
+// row / so / without the other starts / in eight rows: 8192 x 8192 fp32, blocks of rows, both 81.3 / 76.4 / 85.6 / 80.8, 16384 x 8192 bf16 111.9 /
+// 106.4 / 133 / 111, 16384 x 4096 fp32 in squares 73.6 / 73.3 / 87.1 / 76.7, 300 x 30000 bf16 12.1 / 11.2 / 11.1 / 11.2.
+constexpr uint32_t kTileRows = 4, kXcds = 8;
+__device__ __forceinline__ void place_of_tile(uint32_t b, uint32_t count, uint32_t across, int64_t& row, int64_t& col)
+{
+    const uint32_t xcd = b % kXcds, least = count / kXcds, more = count % kXcds, mine = least + (xcd < more);
+    uint32_t i = b / kXcds + (uint32_t)((uint64_t)mine * xcd / kXcds);
+    if (i >= mine) i -= mine;
+    const uint32_t t = xcd * least + (xcd < more ? xcd : more) + i;
+    const uint32_t band = t / (kTileRows * across), in = t - band * kTileRows * across, under = count / across - band * kTileRows;
+    const uint32_t height = under < kTileRows ? under : kTileRows;
+    row = band * kTileRows + in % height;
+    col = in / height;
+}
+
+// LARGE: the outputs do not stay in the memory-side cache for whoever reads them next.  Their stores pass it by then.  us, ordinary / so: 32768 x 8192
+// fp32 in squares, both 316 / 287, 16384 x 8192 bf16 114 / 102; but quantisation and product of 4096 x 4096 (x 4096) 70 / 75.
 constexpr int64_t kLargeBytes = (int64_t)96 << 20;
 template <int DT, bool LARGE>
 __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
@@ -27,9 +43,8 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
     __shared__ __align__(16) uint8_t s_turned[kTile * kTile];
 
     const int t = threadIdx.x, o = t & 15, g = t >> 4, wave = t >> 6;
-    const int64_t tile_col = blockIdx.x % a.tiles_across;
-    int64_t tile_row = blockIdx.x / a.tiles_across;
-    if (LARGE && a.turned) tile_row = (tile_row + tile_col) % (gridDim.x / a.tiles_across);
+    int64_t tile_row, tile_col;
+    place_of_tile(blockIdx.x, gridDim.x, a.tiles_across, tile_row, tile_col);
     const auto put = [](auto x, auto* at) {
         if constexpr (LARGE) __builtin_nontemporal_store(x, at);
         else *at = x;
