@@ -12,7 +12,8 @@ namespace zi {
 // A workgroup takes a tile of 128 x 128, which holds whole blocks of every kind, so x is read once whatever is wanted.
 // A thread has 8 x 8 elements in registers; 16 threads (a row of lanes) have a tile's row, so the largest of a row's
 // block comes from its lanes and that of a column's block from the thread's own rows, two steps over lanes and four
-// wavefronts.  The transposed numbers pass through LDS, which makes rows of 128 bytes of them.
+// wavefronts.  The transposed numbers pass through LDS, which makes rows of 128 bytes of them.  16384 x 4096 fp32 in squares, both 73 us (403 MB, 5.5 TB/s);
+// 8191 x 8192 bf16, blocks of rows, both 55 us (269 MB, 4.9 TB/s, with 6 MB more of scales that were written in pieces); one row of 1000 3.8 us.
 constexpr int kTile = kFp8Block;
 
 // Each XCD has a run of tiles that goes down four rows of tiles before the next column, so that its L2 joins the bytes that neighbours write
@@ -155,7 +156,10 @@ hipError_t launch_fp8_quantize(const QuantizeArgs& a, int dtype, hipStream_t s)
 
 // ---- root-mean-square norm ------------------------------------------------------------------------------------
 
-// T threads have a row, V octets each: octet v * T + t.  16 lanes have a block of 128 columns.
+// One pass: h stays in registers while its squares are summed in fp32 (lanes, then wavefronts in their order), so x and the residual are read once and
+// every output is written once.  T threads have a row, V octets each: octet v * T + t.  16 lanes have a block of 128 columns; its scale is that of the
+// unrounded y, which is rounded to 8 bits directly.  Bound by memory: 16384 x 8192 bf16 with everything 202 us (1209 MB, 6.0 TB/s, a plain copy 6.7); one
+// row of 4096 3.3 us, most of it the way to memory and back twice.
 template <int DT, int T, int V, bool RAGGED>
 __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
 {
@@ -315,6 +319,7 @@ struct BackwardRow {
     }
 };
 
+// Bound by memory: 16384 x 4096 bf16 with dsum 91 us (537 MB, 5.9 TB/s) and 4.8 us for the shares of dgamma.
 // A workgroup goes over rows a grid apart and keeps its columns' share of dgamma in registers; the shares of all
 // workgroups are added by a second kernel in their order.  The next row's loads go out before this row's sum is known (16384 x 4096
 // with dsum 123 -> 97 us).  MEANS: rows that do not fit one workgroup's registers (is_cut) are cut, and means of whole rows come from a kernel in
@@ -387,7 +392,8 @@ __global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_
     }
 }
 
-// dgamma of 16 columns: P rows of threads take every Pth share each, and are added in a fixed order.
+// dgamma of 16 columns: P rows of threads take every Pth share each, and are added in a fixed order.  Bound by latency: 256 shares of 4096 columns
+// 4.8 us (4.2 MB), 333 of 1000 4.2.
 template <int DT, int P>
 __global__ __launch_bounds__(16 * P) void rms_norm_dgamma_kernel(const float* partials, int count, int64_t cols, void* dgamma, int accumulate)
 {

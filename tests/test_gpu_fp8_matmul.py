@@ -190,3 +190,34 @@ def test_the_gradients_of_a_layer():
                             (float((dw.double() * u).sum()), (loss(x.double(), w.double() + u) - loss(x.double(), w.double() - u)) / 2, u)):
         scale = float(size.norm()) * float((dx if size is v else dw).double().norm())
         assert abs(got - diff) <= 2.0 ** -4 / 3 ** 0.5 * 2 ** 0.5 * scale
+
+
+# Products of each size of tile larger than the smallest (64 x 128, 128 x 128 with four and two steps in LDS, 256 x 128, 256 x 256): ends on every side,
+# k that ends inside a block, with a block inside a group of four, and with a group.
+TILES = [(1290, 3000, 384), (1290, 3001, 1667), (1290, 1544, 4001), (2049, 1000, 4001), (2500, 1544, 200), (2049, 2047, 1000), (1001, 4099, 4001),
+         (2049, 2047, 4001), (1290, 3500, 4224), (2049, 6001, 1667), (3001, 4099, 2560), (3001, 4100, 3000)]
+
+
+@pytest.mark.parametrize("m,n,k", TILES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_every_tile_is_exact(m, n, k, dtype):
+    a, b = _whole(m, k, 1, 30), _whole(n, k, 128, 40)
+    exact = _exact(a, b)
+    assert torch.equal(_call(a, b, dtype), exact.to(dtype))
+    c = torch.randint(-8, 9, (m, n), generator=torch.Generator(device="cuda:0").manual_seed(50), device="cuda:0").to(dtype)
+    want = (exact + c.double()).to(dtype)
+    assert torch.equal(_call(a, b, dtype, c=c, pad=3), want)
+    assert torch.equal(_call(a, b, dtype, c=c, inplace=True), want)
+
+
+@pytest.mark.parametrize("m,n,k", [(1290, 3001, 1667), (1290, 1544, 4001), (1001, 4099, 4001), (3001, 4100, 3000)])
+def test_every_tile_keeps_nan_to_its_row_and_gives_the_same_bits(m, n, k):
+    a, b = _normal(m, k, 1, 31), _normal(n, k, 128, 41)
+    first = _call(a, b, torch.bfloat16)
+    for _ in range(3):
+        assert torch.equal(_call(a, b, torch.bfloat16), first)
+    a.data[m - 2, k - 1] = 0x7F
+    spoilt = _call(a, b, torch.bfloat16)
+    assert bool(spoilt[m - 2].isnan().all())
+    spoilt[m - 2] = first[m - 2]
+    assert torch.equal(spoilt, first)
