@@ -393,16 +393,27 @@ __global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_
 }
 
 // dgamma of 16 columns: P rows of threads take every Pth share each, and are added in a fixed order.  Bound by latency: 256 shares of 4096 columns
-// 4.8 us (4.2 MB), 333 of 1000 4.2.
+// 4.8 us (4.2 MB).  Eight shares' loads go out at a time (backward pass of 13683 x 152 18.4 -> 14.3, 8192 x 1024 21.3 -> 18.8).
 template <int DT, int P>
 __global__ __launch_bounds__(16 * P) void rms_norm_dgamma_kernel(const float* partials, int count, int64_t cols, void* dgamma, int accumulate)
 {
+    constexpr int kAtOnce = 8;
     __shared__ float s_sum[P][16];
     const int in = threadIdx.x & 15, part = threadIdx.x >> 4;
     const int64_t col = (int64_t)blockIdx.x * 16 + in;
     float sum = 0.0f;
     if (col < cols)
-        for (int i = part; i < count; i += P) sum += partials[(int64_t)i * cols + col];
+        for (int first = part; first < count; first += kAtOnce * P) {
+            float x[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                const int at = first + i * P;
+                x[i] = partials[(int64_t)(at < count ? at : part) * cols + col];
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                if (first + i * P < count) sum += x[i];
+        }
     s_sum[part][in] = sum;
     __syncthreads();
     if (part != 0 || col >= cols) return;
@@ -491,7 +502,13 @@ template <int DT>
 void launch_norm_of(const RmsNormArgs& a, hipStream_t s)
 {
     const LaunchNorm f{a, s};
-    if (a.a.cols <= 1024 * 16) with_row_shape<DT>(a.a.cols, f);
+    // Of 8193 to 16384 columns, 1024 threads with two octets leave room for one workgroup on a compute unit, 512 with three or four for two; they need more
+    // turns for a row, which counts where each unit has one row at most.  us, 1024 / 512: 16351 x 8208 fp16 260 / 182, 12000 x 11000 219 / 175, 10483 x 12803
+    // 330 / 282, 8192 x 16384 220 / 219; but 1 x 16000 4.8 / 6.1.
+    const bool many = a.a.rows > 256;
+    if (many && a.a.cols > 512 * 16 && a.a.cols <= 512 * 24) f.template operator()<DT, 512, 3>();
+    else if (many && a.a.cols > 512 * 24 && a.a.cols <= 512 * 32) f.template operator()<DT, 512, 4>();
+    else if (a.a.cols <= 1024 * 16) with_row_shape<DT>(a.a.cols, f);
     else if (a.a.cols <= 1024 * 32) f.template operator()<DT, 1024, 4>();
     else f.template operator()<DT, 1024, 8>();
 }
