@@ -17,8 +17,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_of_2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_of_4 __attribute__((ext_vector_type(4), aligned(4)));
 
-// How an octet comes that a row ends in: there is none; it is the row's last eight elements, one load for all lanes alike, which settle() moves down
-// where they are used (where they are loaded it would wait for them: backward pass of 10743 x 2509 154 us against 102); its elements one by one.
+// How an octet comes that a row ends in: there is none; it is the row's last eight elements (of eight at least), one load for all lanes alike, which settle()
+// moves down where they are used (where they are loaded it would wait for them: backward pass of 10743 x 2509 154 us against 102); its elements one by one.
 enum class Ends { kWhole, kMoved, kApart };
 
 // Eight elements of a row.  Rows need only be aligned to their element: the hardware takes such vectors as they are.
@@ -31,15 +31,11 @@ struct Octet {
 
     // The octet at `at`, of which a row of `cols` has `left` more elements (none or less than none: zeros); zeros behind its end.
     template <Ends ENDS>
-    __device__ __forceinline__ void load(const void* base, int64_t at, int left, int64_t cols)
+    __device__ __forceinline__ void load(const void* base, int64_t at, int left)
     {
         int past = 0;
         if constexpr (ENDS == Ends::kMoved) {
             past = left >= 8 ? 0 : 8 - left;
-            if (cols < 8) {
-                load_short(base, at, left);
-                return;
-            }
         } else if (left < 8) {
             if (ENDS == Ends::kApart) load_short(base, at, left);
             else clear();
@@ -54,10 +50,10 @@ struct Octet {
         }
     }
     template <Ends ENDS>
-    __device__ __forceinline__ void settle(int left, int64_t cols)
+    __device__ __forceinline__ void settle(int left)
     {
         if constexpr (ENDS == Ends::kMoved)
-            if (left < 8 && cols >= 8) {
+            if (left < 8) {
                 if (left > 0) drop(8 - left);
                 else clear();
             }

@@ -389,8 +389,12 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
                 Octet<OUT> c;
                 c.clear();
                 if (row < p.m) {
-                    c.template load<Ends::kMoved>(p.c, row * p.d_ld + col, valid, p.n);
-                    c.template settle<Ends::kMoved>(valid, p.n);
+                    if (p.n < 8) {
+                        c.template load<Ends::kApart>(p.c, row * p.d_ld + col, valid);
+                    } else {
+                        c.template load<Ends::kMoved>(p.c, row * p.d_ld + col, valid);
+                        c.template settle<Ends::kMoved>(valid);
+                    }
                 }
                 *reinterpret_cast<u32x4*>(chunk(r, own_chunk)) = u32x4{c.w[0], c.w[1], c.w[2], c.w[3]};
             }

@@ -35,9 +35,11 @@ __device__ __forceinline__ void place_of_tile(uint32_t b, uint32_t count, uint32
 
 // LARGE: the outputs do not stay in the memory-side cache for whoever reads them next.  Their stores pass it by then.  us, ordinary / so: 32768 x 8192
 // fp32 in squares, both 316 / 287, 16384 x 8192 bf16 114 / 102; but quantisation and product of 4096 x 4096 (x 4096) 70 / 75.
+// Large outputs of fp32 keep to two workgroups on a compute unit, three where registers allow them: 16384 x 4096 in squares 72.8 / 77.1, 32768 x 8192 280 /
+// 296, but 8192 x 8192 in blocks of rows 76.4 / 73.3, and with small outputs 4096 x 4096 20.5 / 20.0.
 constexpr int64_t kLargeBytes = (int64_t)96 << 20;
 template <int DT, bool LARGE>
-__global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, LARGE && DT == ZI_FP32 ? 2 : 8))) void fp8_quantize_kernel(const QuantizeArgs a)
 {
     __shared__ uint32_t s_col[4][kTile / 8 * Octet<DT>::kWords];
     __shared__ uint32_t s_all[4];
@@ -55,14 +57,21 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantizeArgs a)
     const int in_row = left >= 8 ? 8 : left > 0 ? (int)left : 0, in_row_or_less = left >= 8 ? 8 : (int)left;
 
     Octet<DT> x[8];
+    const auto load_rows = [&](auto ends) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i].clear();
-        if (row0 + i < a.rows) x[i].template load<Ends::kMoved>(a.x, (row0 + i) * a.ld + col0, in_row_or_less, a.cols);
-    }
-    if (in_row < 8) {
+        for (int i = 0; i < 8; ++i) {
+            x[i].clear();
+            if (row0 + i < a.rows) x[i].template load<decltype(ends)::value>(a.x, (row0 + i) * a.ld + col0, in_row_or_less);
+        }
+    };
+    if (a.cols < 8) {
+        load_rows(std::integral_constant<Ends, Ends::kApart>());
+    } else {
+        load_rows(std::integral_constant<Ends, Ends::kMoved>());
+        if (in_row < 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i].template settle<Ends::kMoved>(in_row_or_less, a.cols);
+            for (int i = 0; i < 8; ++i) x[i].template settle<Ends::kMoved>(in_row_or_less);
+        }
     }
 
     constexpr int kWords = Octet<DT>::kWords;
@@ -160,12 +169,11 @@ hipError_t launch_fp8_quantize(const QuantizeArgs& a, int dtype, hipStream_t s)
 // every output is written once.  T threads have a row, V octets each: octet v * T + t.  16 lanes have a block of 128 columns; its scale is that of the
 // unrounded y, which is rounded to 8 bits directly.  Bound by memory: 16384 x 8192 bf16 with everything 202 us (1209 MB, 6.0 TB/s, a plain copy 6.7); one
 // row of 4096 3.3 us, most of it the way to memory and back twice.
-template <int DT, int T, int V, bool RAGGED>
+template <int DT, int T, int V, Ends ENDS>
 __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
 {
     __shared__ float s_sum[T / 64];
     constexpr bool kAllFirst = V <= 2;          // all loads in front of what uses them, while there are registers for them
-    constexpr Ends kEnds = !RAGGED ? Ends::kWhole : V <= 4 ? Ends::kMoved : Ends::kApart;      // (eight octets leave no registers for moving)
     const zi_rms_norm_args& a = k.a;
     const int cols = (int)a.cols, own = (int)threadIdx.x * 8;                    // (columns are at most 65536)
     const auto column = [&](int v) { return own + v * T * 8; };
@@ -176,23 +184,23 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = column(v);
-            h[v].template load<kEnds>(a.x, row * a.x_ld + col, valid(v), a.cols);
-            if constexpr (kAllFirst) gammas[v].template load<kEnds>(a.gamma, col, valid(v), a.cols);
+            h[v].template load<ENDS>(a.x, row * a.x_ld + col, valid(v));
+            if constexpr (kAllFirst) gammas[v].template load<ENDS>(a.gamma, col, valid(v));
         }
         Octet<DT> residual[kAllFirst ? V : 1];
         if (kAllFirst && a.residual) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) residual[kAllFirst ? v : 0].template load<kEnds>(a.residual, row * a.residual_ld + column(v), valid(v), a.cols);
+            for (int v = 0; v < V; ++v) residual[kAllFirst ? v : 0].template load<ENDS>(a.residual, row * a.residual_ld + column(v), valid(v));
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v].template settle<kEnds>(valid(v), a.cols);
+        for (int v = 0; v < V; ++v) h[v].template settle<ENDS>(valid(v));
         if (a.residual) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int col = column(v);
                 Octet<DT>& r = residual[kAllFirst ? v : 0];
-                if constexpr (!kAllFirst) r.template load<kEnds>(a.residual, row * a.residual_ld + col, valid(v), a.cols);
-                r.template settle<kEnds>(valid(v), a.cols);
+                if constexpr (!kAllFirst) r.template load<ENDS>(a.residual, row * a.residual_ld + col, valid(v));
+                r.template settle<ENDS>(valid(v));
                 float f[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = h[v].get(j) + r.get(j);
@@ -212,8 +220,8 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
             for (int v = 0; v < V; ++v) {
                 const int col = column(v);
                 Octet<DT>& gamma = gammas[kAllFirst ? v : 0];
-                if constexpr (!kAllFirst) gamma.template load<kEnds>(a.gamma, col, valid(v), a.cols);
-                gamma.template settle<kEnds>(valid(v), a.cols);
+                if constexpr (!kAllFirst) gamma.template load<ENDS>(a.gamma, col, valid(v));
+                gamma.template settle<ENDS>(valid(v));
                 float y[8];
                 uint32_t most = 0;
 #pragma unroll
@@ -250,9 +258,8 @@ __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
 // ---- its backward pass ----------------------------------------------------------------------------------------
 
 // What a thread has of a row: V octets T threads apart, from column `first` on.
-template <int DT, int T, int V, bool RAGGED>
+template <int DT, int T, int V, Ends ENDS>
 struct BackwardRow {
-    static constexpr Ends kEnds = RAGGED ? Ends::kMoved : Ends::kWhole;
     Octet<DT> dy[V], h[V], add[V];
     float rstd;
     static __device__ __forceinline__ int column(int first, int v) { return first + (v * T + (int)threadIdx.x) * 8; }
@@ -266,23 +273,23 @@ struct BackwardRow {
         rstd = a.rstd[row];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            dy[v].template load<kEnds>(a.dy, row * a.dy_ld + column(first, v), valid(a, first, v), a.cols);
-            h[v].template load<kEnds>(a.h, row * a.h_ld + column(first, v), valid(a, first, v), a.cols);
+            dy[v].template load<ENDS>(a.dy, row * a.dy_ld + column(first, v), valid(a, first, v));
+            h[v].template load<ENDS>(a.h, row * a.h_ld + column(first, v), valid(a, first, v));
         }
     }
     __device__ __forceinline__ void load_dsum(const zi_rms_norm_backward_args& a, int64_t row, int first)
     {
         if (!a.dsum) return;
 #pragma unroll
-        for (int v = 0; v < V; ++v) add[v].template load<kEnds>(a.dsum, row * a.dsum_ld + column(first, v), valid(a, first, v), a.cols);
+        for (int v = 0; v < V; ++v) add[v].template load<ENDS>(a.dsum, row * a.dsum_ld + column(first, v), valid(a, first, v));
     }
     __device__ __forceinline__ void settle(const zi_rms_norm_backward_args& a, int first)
     {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            dy[v].template settle<kEnds>(valid(a, first, v), a.cols);
-            h[v].template settle<kEnds>(valid(a, first, v), a.cols);
-            if (a.dsum) add[v].template settle<kEnds>(valid(a, first, v), a.cols);
+            dy[v].template settle<ENDS>(valid(a, first, v));
+            h[v].template settle<ENDS>(valid(a, first, v));
+            if (a.dsum) add[v].template settle<ENDS>(valid(a, first, v));
         }
     }
     __device__ __forceinline__ float dot(const Octet<DT> (&gamma)[V]) const
@@ -324,10 +331,10 @@ struct BackwardRow {
 // workgroups are added by a second kernel in their order.  The next row's loads go out before this row's sum is known (16384 x 4096
 // with dsum 123 -> 97 us).  MEANS: rows that do not fit one workgroup's registers (is_cut) are cut, and means of whole rows come from a kernel in
 // front (rms_norm_means_kernel), so that dy and h are read twice.
-template <int DT, int T, int V, bool MEANS, bool RAGGED>
+template <int DT, int T, int V, bool MEANS, Ends ENDS>
 __global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_backward_args a, float* partials, const float* means, uint32_t cuts)
 {
-    using Row = BackwardRow<DT, T, V, RAGGED>;
+    using Row = BackwardRow<DT, T, V, ENDS>;
     constexpr bool kAhead = T < 1024;          // dsum too; 1024 threads have 128 registers each, and no room for it
     __shared__ float s_sum[2][T / 64];
     const uint32_t group = MEANS ? blockIdx.x / cuts : blockIdx.x, groups = MEANS ? gridDim.x / cuts : gridDim.x;
@@ -339,8 +346,8 @@ __global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_
     if constexpr (kAhead) now.load_dsum(a, group, first);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        gamma[v].template load<Row::kEnds>(a.gamma, Row::column(first, v), Row::valid(a, first, v), a.cols);
-        gamma[v].template settle<Row::kEnds>(Row::valid(a, first, v), a.cols);
+        gamma[v].template load<ENDS>(a.gamma, Row::column(first, v), Row::valid(a, first, v));
+        gamma[v].template settle<ENDS>(Row::valid(a, first, v));
     }
     int turn = 0;
     for (int64_t row = group; row < a.rows; row += groups, turn ^= 1) {
@@ -366,10 +373,10 @@ __global__ __launch_bounds__(T) void rms_norm_backward_kernel(const zi_rms_norm_
 }
 
 // The mean of u * n of each row.
-template <int DT, bool RAGGED>
+template <int DT, Ends ENDS>
 __global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_backward_args a, float* means)
 {
-    using Row = BackwardRow<DT, 1024, 2, RAGGED>;
+    using Row = BackwardRow<DT, 1024, 2, ENDS>;
     __shared__ float s_sum[16];
     zi_rms_norm_backward_args b = a;             // without dsum, which is not loaded
     b.dsum = nullptr;
@@ -380,10 +387,10 @@ __global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_
             Octet<DT> gamma[2];
             r.load(a, row, first);
 #pragma unroll
-            for (int v = 0; v < 2; ++v) gamma[v].template load<Row::kEnds>(a.gamma, Row::column(first, v), Row::valid(a, first, v), a.cols);
+            for (int v = 0; v < 2; ++v) gamma[v].template load<ENDS>(a.gamma, Row::column(first, v), Row::valid(a, first, v));
             r.settle(b, first);
 #pragma unroll
-            for (int v = 0; v < 2; ++v) gamma[v].template settle<Row::kEnds>(Row::valid(a, first, v), a.cols);
+            for (int v = 0; v < 2; ++v) gamma[v].template settle<ENDS>(Row::valid(a, first, v));
             sum += r.dot(gamma);
         }
         sum = sum_of_group<1024>(sum, s_sum);
@@ -457,8 +464,10 @@ struct LaunchNorm {
     {
         const int64_t most = (int64_t)1 << 20;
         const dim3 grid((unsigned)(a.a.rows < most ? a.a.rows : most)), block(T);
-        if (a.a.cols % 8) hipLaunchKernelGGL((rms_norm_kernel<DT, T, V, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((rms_norm_kernel<DT, T, V, false>), grid, block, 0, s, a);
+        constexpr Ends kRagged = V <= 4 ? Ends::kMoved : Ends::kApart;       // (eight octets leave no registers for moving)
+        if (a.a.cols % 8 == 0) hipLaunchKernelGGL((rms_norm_kernel<DT, T, V, Ends::kWhole>), grid, block, 0, s, a);
+        else if (a.a.cols > 8) hipLaunchKernelGGL((rms_norm_kernel<DT, T, V, kRagged>), grid, block, 0, s, a);
+        else if constexpr (T == 64 && V == 1) hipLaunchKernelGGL((rms_norm_kernel<DT, T, V, Ends::kApart>), grid, block, 0, s, a);
     }
 };
 struct LaunchBackward {
@@ -474,12 +483,15 @@ struct LaunchBackward {
     template <int DT, int T, int V, bool MEANS>
     void launch(unsigned grid, const float* means, unsigned cuts) const
     {
-        if constexpr (T < 1024)
-            if (a.cols % 8) {
-                hipLaunchKernelGGL((rms_norm_backward_kernel<DT, T, V, MEANS, true>), dim3(grid), dim3(T), 0, s, a, partials, means, cuts);
-                return;
-            }
-        hipLaunchKernelGGL((rms_norm_backward_kernel<DT, T, V, MEANS, false>), dim3(grid), dim3(T), 0, s, a, partials, means, cuts);
+        if (a.cols % 8 == 0) return launch_ends<DT, T, V, MEANS, Ends::kWhole>(grid, means, cuts);
+        if constexpr (T == 64 && V == 1)
+            if (a.cols < 8) return launch_ends<DT, T, V, MEANS, Ends::kApart>(grid, means, cuts);
+        if constexpr (T < 1024) launch_ends<DT, T, V, MEANS, Ends::kMoved>(grid, means, cuts);
+    }
+    template <int DT, int T, int V, bool MEANS, Ends ENDS>
+    void launch_ends(unsigned grid, const float* means, unsigned cuts) const
+    {
+        hipLaunchKernelGGL((rms_norm_backward_kernel<DT, T, V, MEANS, ENDS>), dim3(grid), dim3(T), 0, s, a, partials, means, cuts);
     }
     template <int DT>
     void cut() const
@@ -487,8 +499,8 @@ struct LaunchBackward {
         float* means = partials + (int64_t)groups * a.cols;
         const unsigned cuts = (unsigned)((a.cols + kCutCols - 1) / kCutCols);
         const dim3 grid((unsigned)(a.rows < 4096 ? a.rows : 4096)), block(1024);
-        if (a.cols % 8) hipLaunchKernelGGL((rms_norm_means_kernel<DT, true>), grid, block, 0, s, a, means);
-        else hipLaunchKernelGGL((rms_norm_means_kernel<DT, false>), grid, block, 0, s, a, means);
+        if (a.cols % 8) hipLaunchKernelGGL((rms_norm_means_kernel<DT, Ends::kMoved>), grid, block, 0, s, a, means);
+        else hipLaunchKernelGGL((rms_norm_means_kernel<DT, Ends::kWhole>), grid, block, 0, s, a, means);
         launch<DT, kCutThreads, 2, true>(groups * cuts, means, cuts);
     }
     template <int DT>
