@@ -13,7 +13,7 @@ namespace zi {
 // A thread has 8 x 8 elements in registers; 16 threads (a row of lanes) have a tile's row, so the largest of a row's
 // block comes from its lanes and that of a column's block from the thread's own rows, two steps over lanes and four
 // wavefronts.  The transposed numbers pass through LDS, which makes rows of 128 bytes of them.  16384 x 4096 fp32 in squares, both 73 us (403 MB, 5.5 TB/s);
-// 8191 x 8192 bf16, blocks of rows, both 55 us (269 MB, 4.9 TB/s, with 6 MB more of scales that were written in pieces); one row of 1000 3.8 us.
+// 8191 x 8192 bf16, blocks of rows, both 55 us (269 MB, 4.9 TB/s, with 6 MB more of scales that were written in pieces); one row of 1000 3.7 us.
 constexpr int kTile = kFp8Block;
 
 // Each XCD has a run of tiles that goes down four rows of tiles before the next column, so that its L2 joins the bytes that neighbours write
