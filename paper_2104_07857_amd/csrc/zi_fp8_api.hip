@@ -8,7 +8,7 @@ using namespace zi::host;
 
 namespace {
 
-constexpr int64_t kMostRows = (int64_t)1 << 40;     // keeps every product of sizes below 2^63
+constexpr int64_t kMostRows = (int64_t)1 << 40;     // of rows, columns, pitches, and of rows times pitch: extents in bytes stay below 2^43
 constexpr int64_t kMostTiles = (int64_t)1 << 22;    // workgroups of a launch, of up to 1024 threads
 constexpr int64_t kMostPitch = (int64_t)1 << 23;    // of a product's operand: 32-bit offsets reach the 256 rows of a tile
 
@@ -84,6 +84,8 @@ zi_status check_fp8(const zi_fp8_matrix& x, const char* name)
     if (!x.data || !x.scale) return fail(ZI_ERR_INVALID_ARG, "%s: data and scale must not be NULL", name);
     if (zi_status st = check_pitch(x.ld, x.cols, name)) return st;
     if (zi_status st = check_pitch(x.scale_ld, up(x.cols, zi::kFp8Block), name)) return st;
+    if (x.ld > kMostRows / x.rows || x.scale_ld > kMostRows / up(x.rows, x.block_rows))
+        return fail(ZI_ERR_UNSUPPORTED, "%s has more than 2^40 elements", name);
     if (x.ld % 16 || x.scale_ld % 4)
         return fail(ZI_ERR_ALIGNMENT, "%s: ld must be a multiple of 16, scale_ld of 4", name);
     if (!aligned(x.data, 16) || !aligned(x.scale, 4))
@@ -175,8 +177,7 @@ extern "C" zi_status zi_fp8_matmul(const zi_fp8_matrix* a, const zi_fp8_matrix* 
     if (!d) return fail(ZI_ERR_INVALID_ARG, "d is NULL");
     if (!aligned(d, 2) || !aligned(c, 2)) return fail(ZI_ERR_ALIGNMENT, "d and c must be 2-byte aligned");
     if (zi_status st = check_pitch(ldd, n, "d")) return st;
-    if (m > kMostRows / ldd || (k > 0 && (m > kMostRows / a->ld || n > kMostRows / b->ld)))
-        return fail(ZI_ERR_UNSUPPORTED, "an operand of more than 2^40 elements");
+    if (m > kMostRows / ldd) return fail(ZI_ERR_UNSUPPORTED, "d has more than 2^40 elements");
     if (up(n, 16) > kMostTiles || up(m, 128) > kMostTiles / up(n, 128))
         return fail(ZI_ERR_UNSUPPORTED, "D of more than 2^36 elements, or b of more than 2^26 rows");
     if (k > 0 && (a->ld >= kMostPitch || b->ld >= kMostPitch || a->scale_ld >= kMostPitch || b->scale_ld >= kMostPitch))
