@@ -10,6 +10,7 @@ namespace {
 
 constexpr int64_t kMostRows = (int64_t)1 << 40;     // of rows, columns, pitches, and of rows times pitch: extents in bytes stay below 2^43
 constexpr int64_t kMostTiles = (int64_t)1 << 22;    // workgroups of a launch, of up to 1024 threads
+constexpr int64_t kMostSquares = ((int64_t)1 << 24) - 1;     // tiles of the quantisation, of 256 threads: a launch has less than 2^32
 constexpr int64_t kMostPitch = (int64_t)1 << 23;    // of a product's operand: 32-bit offsets reach the 256 rows of a tile
 
 bool bad_real(int32_t dtype, bool fp32) { return dtype != ZI_BF16 && dtype != ZI_FP16 && !(fp32 && dtype == ZI_FP32); }
@@ -123,8 +124,9 @@ extern "C" zi_status zi_fp8_quantize(const void* x, int32_t dtype, int64_t rows,
     if (!x) return fail(ZI_ERR_INVALID_ARG, "x is NULL");
     if (!aligned(x, (size_t)bytes_of(dtype))) return fail(ZI_ERR_ALIGNMENT, "x must be aligned to its element");
     if (zi_status st = check_pitch(ld, cols, "x")) return st;
-    if (rows > kMostRows / cols || up(rows, zi::kFp8Block) > (1 << 24) / up(cols, zi::kFp8Block) || rows > kMostRows / ld)
-        return fail(ZI_ERR_UNSUPPORTED, "more than 2^24 tiles of 128 x 128");
+    if (rows > kMostRows / ld) return fail(ZI_ERR_UNSUPPORTED, "x has more than 2^40 elements");
+    if (up(rows, zi::kFp8Block) > kMostSquares / up(cols, zi::kFp8Block))
+        return fail(ZI_ERR_UNSUPPORTED, "x has 2^24 tiles of 128 x 128 or more");
     Arrays all;
     all.add("x", x, rows, cols * bytes_of(dtype), ld * bytes_of(dtype), false);
     if (out) add_fp8(all, *out, "out's data", "out's scale", true);

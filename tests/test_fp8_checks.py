@@ -39,3 +39,18 @@ def test_rows_of_scales_are_what_counts_for_them(field, pitch):
         with pytest.raises(zi.ZiError) as e:
             zi.zi_fp8_quantize(x, BF16, 100, 8, 8, m)
         assert e.value.status in (zi.ZI_ERR_HIP, INVALID) and "2^40" not in e.value.message
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 31, 1), ((1 << 31) - 127, 1), (1 << 30, 129), (1 << 19, 1 << 19)])
+def test_a_launch_of_two_to_the_32_threads_is_refused(rows, cols):
+    """2^24 tiles of 256 threads are one thread more than a launch has."""
+    _refused(UNSUPPORTED, "tiles", zi.zi_fp8_quantize, 16 * GIB, BF16, rows, cols, cols, None, _at(cols, rows))
+    _refused(UNSUPPORTED, "tiles", zi.zi_fp8_quantize, 16 * GIB, BF16, rows, cols, cols, _at(rows, cols))
+
+
+def test_one_tile_less_is_not():
+    rows = (1 << 31) - 128
+    x = _half(4, 4)
+    with pytest.raises(zi.ZiError) as e:
+        zi.zi_fp8_quantize(x, BF16, rows, 1, 1, None, _at(1, rows))
+    assert e.value.status in (zi.ZI_ERR_HIP, INVALID) and "tiles" not in e.value.message
