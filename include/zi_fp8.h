@@ -23,8 +23,9 @@
  *
  * Conventions are those of zi.h: plain addresses, statuses and zi_last_error(), nothing kept after a call, everything
  * checked before anything is launched, asynchronous on hip_stream, no allocation (calls can be captured into a
- * graph).  Sizes of zero are valid.  An output overlaps no input and no other output, except where in-place use is
- * said to work; then both have the same address and pitch.  The results of a call do not depend on the order in which
+ * graph).  Sizes of zero are valid.  An output shares no byte with an input or another output, except where in-place use is
+ * said to work; then both have the same address and pitch.  Columns or rows of one buffer may be input and output of a call,
+ * if their pitches are the same or one is a multiple of the other; an output in 8 bits has its rows' pitches to itself.  The results of a call do not depend on the order in which
  * the GPU runs its workgroups.
  */
 #ifndef ZI_FP8_H
@@ -42,10 +43,11 @@ extern "C" {
 #define ZI_FP8_BLOCK 128
 
 /*
- * A matrix in 8 bits.  data: rows * ld bytes, 16-byte aligned, ld a multiple of 16 and at least cols; what rows hold
- * from column cols on is never used (zi_fp8_quantize and zi_rms_norm write zeros up to the next multiple of 8).
- * scale: ceil(rows / block_rows) rows of scale_ld bytes, 4-byte aligned, scale_ld a multiple of 4 and at least
- * ceil(cols / 128).  block_rows: 1 or 128.
+ * A matrix in 8 bits.  data: rows of cols bytes and up to the next multiple of 16, each ld bytes from the one before, 16-byte
+ * aligned, ld a multiple of 16 and at least cols; what these bytes hold from column cols on is never used (zi_fp8_quantize
+ * writes zeros up to the next multiple of 8, or 16 in `turned`; zi_rms_norm of 8).  scale: ceil(rows / block_rows) rows of
+ * ceil(cols / 128) bytes and up to the next multiple of 4, scale_ld bytes apart, 4-byte aligned, scale_ld a multiple of 4 and at
+ * least ceil(cols / 128); the bytes behind the last block's are read, and neither used nor written.  block_rows: 1 or 128.
  */
 typedef struct {
     void* data;

@@ -1,6 +1,8 @@
 // C-ABI entry points of the 8-bit operators: argument checks and launches.  See include/zi_fp8.h for the contract.
 #include <hip/hip_runtime.h>
 
+#include <numeric>
+
 #include "zi_fp8_internal.h"
 #include "zi_host.h"
 
@@ -24,14 +26,27 @@ zi_status check_size(int64_t n, const char* name)
     return ZI_OK;
 }
 
-// One array of a call: its place, its extent in bytes and whether the call writes it.
+// One array of a call: its place, its rows, its extent in bytes and whether the call writes it.
 struct Range {
     const char* name;
     const void* at;
+    int64_t rows, row_bytes;
     int64_t pitch;         // in bytes
     int64_t bytes;
     bool written;
 };
+
+// Whether two arrays may share a byte.  Where the place of a row within a period that divides both pitches is apart from the other's, they lie between each
+// other's rows, as columns of one buffer do; a single row has any period.  Exact for rows of one pitch; of different pitches, all that share are found.
+bool may_share(const Range& x, const Range& y)
+{
+    const uintptr_t a = (uintptr_t)x.at, b = (uintptr_t)y.at;
+    if (a >= b + (uintptr_t)y.bytes || b >= a + (uintptr_t)x.bytes) return false;
+    if (x.rows == 1 && y.rows == 1) return true;
+    const uint64_t period = x.rows == 1 ? y.pitch : y.rows == 1 ? x.pitch : std::gcd(x.pitch, y.pitch);
+    const uint64_t from = b >= a ? (b - a) % period : (period - (a - b) % period) % period;     // of y's rows, x's begin at 0
+    return from < (uint64_t)x.row_bytes || from + (uint64_t)y.row_bytes > period;
+}
 
 // The arrays of a call: each has to be the GPU's to reach, and an output may share no byte with another array, but for
 // those of the same place and pitch that the call takes in place.
@@ -40,11 +55,12 @@ struct Arrays {
     int count = 0;
     uint32_t in_place[12] = {};   // by index, the arrays that it may coincide with
 
-    int add(const char* name, const void* at, int64_t rows, int64_t row_bytes, int64_t pitch, bool written, uint32_t same = 0)
+    // `own`: bytes that a row has to itself, if that is more than it holds.
+    int add(const char* name, const void* at, int64_t rows, int64_t row_bytes, int64_t pitch, bool written, uint32_t same = 0, int64_t own = 0)
     {
         if (!at || rows <= 0 || row_bytes <= 0) return 31;
         in_place[count] = same;
-        list[count] = {name, at, pitch, (rows - 1) * pitch + row_bytes, written};
+        list[count] = {name, at, rows, own > row_bytes ? own : row_bytes, pitch, (rows - 1) * pitch + row_bytes, written};
         return count++;
     }
     zi_status check() const
@@ -54,10 +70,8 @@ struct Arrays {
                 return fail(ZI_ERR_INVALID_ARG, "%s (%lld bytes) is no array", list[i].name, (long long)list[i].bytes);
             for (int j = 0; j < i; ++j) {
                 const Range &x = list[i], &y = list[j];
-                if (!x.written && !y.written) continue;
-                const uintptr_t a = (uintptr_t)x.at, b = (uintptr_t)y.at;
-                if (a >= b + (uintptr_t)y.bytes || b >= a + (uintptr_t)x.bytes) continue;
-                const bool same = a == b && x.pitch == y.pitch && (((in_place[i] >> j) | (in_place[j] >> i)) & 1u);
+                if ((!x.written && !y.written) || !may_share(x, y)) continue;
+                const bool same = x.at == y.at && x.pitch == y.pitch && (((in_place[i] >> j) | (in_place[j] >> i)) & 1u);
                 if (!same) return fail(ZI_ERR_INVALID_ARG, "%s and %s overlap", y.name, x.name);
             }
         }
@@ -97,8 +111,9 @@ zi_status check_fp8(const zi_fp8_matrix& x, const char* name)
 void add_fp8(Arrays& all, const zi_fp8_matrix& x, const char* data, const char* scale, bool written)
 {
     if (x.cols == 0) return;
-    all.add(data, x.data, x.rows, x.ld, x.ld, written);
-    all.add(scale, x.scale, up(x.rows, x.block_rows), x.scale_ld, x.scale_ld, written);
+    // (rows are read and written in vectors of up to 16 bytes, their scales read by fours; one that is written has its pitch to itself)
+    all.add(data, x.data, x.rows, up(x.cols, 16) * 16, x.ld, written, 0, written ? x.ld : 0);
+    all.add(scale, x.scale, up(x.rows, x.block_rows), up(x.cols, 4 * zi::kFp8Block) * 4, x.scale_ld, written, 0, written ? x.scale_ld : 0);
 }
 
 }  // namespace
