@@ -463,15 +463,40 @@ def zi_pinned_free(ptr) -> int:
 
 # ---- the 8-bit operators of include/zi_fp8.h ------------------------------------------------
 
-def _pitch(x) -> int:
-    """Elements from row to row of a matrix (torch tensor or numpy array) whose columns are neighbours."""
+def _rows_at(x, rows: int, cols: int, itemsize: Optional[int], name: str):
+    """Address and pitch of a matrix (None: 0), of which rows x cols elements are used."""
+    if x is None:
+        return None, 0
     if hasattr(x, "data_ptr"):
-        rows, cols, (pitch, step) = *x.shape, x.stride()
+        at, shape, strides, size = x.data_ptr(), x.shape, x.stride(), x.element_size()
     else:
-        rows, cols, (pitch, step) = *x.shape, (s // x.itemsize for s in x.strides)
-    if step != 1 and cols > 1:
-        raise ValueError("the columns of a matrix have to be neighbours in memory")
-    return int(pitch) if rows > 1 else max(int(pitch), int(cols))
+        size = x.itemsize
+        at, shape, strides = x.ctypes.data, x.shape, [s // size for s in x.strides]
+    if len(shape) != 2 or shape[0] < rows or shape[1] < cols:
+        raise ValueError(f"{name} is {tuple(shape)}: {rows} rows of {cols} are wanted")
+    if size != itemsize and itemsize is not None:
+        raise ValueError(f"{name} has elements of {size} bytes: {itemsize} are wanted")
+    if strides[1] != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: the columns of a matrix have to be neighbours in memory")
+    return at, strides[0] if shape[0] > 1 else max(strides[0], shape[1])
+
+
+def _vector_at(x, n: int, itemsize: Optional[int], name: str):
+    """Address of n elements in a row (an address is the caller's word for them)."""
+    if x is None or isinstance(x, int):
+        return x
+    if hasattr(x, "data_ptr"):
+        at, count, size, whole = x.data_ptr(), x.numel(), x.element_size(), x.is_contiguous()
+    else:
+        at, count, size, whole = x.ctypes.data, x.size, x.itemsize, x.flags.c_contiguous
+    if count < n or not whole:
+        raise ValueError(f"{name}: {n} elements that are neighbours in memory are wanted")
+    if size != itemsize and itemsize is not None:
+        raise ValueError(f"{name} has elements of {size} bytes: {itemsize} are wanted")
+    return at
+
+
+_BYTES_OF = {ZI_BF16: 2, ZI_FP16: 2, ZI_FP32: 4}       # (the library refuses other types)
 
 
 def fp8_layout(rows: int, cols: int, block_rows: int = 1):
@@ -483,28 +508,37 @@ def fp8_layout(rows: int, cols: int, block_rows: int = 1):
 def make_fp8_matrix(data, scale, rows: int, cols: int, block_rows: int = 1, ld: Optional[int] = None,
                     scale_ld: Optional[int] = None) -> zi_fp8_matrix:
     """A zi_fp8_matrix over two byte arrays (torch tensors or numpy arrays of two dimensions; addresses with ld and scale_ld)."""
-    return zi_fp8_matrix(_addr(data), _addr(scale), int(rows), int(cols), int(_pitch(data) if ld is None else ld),
-                         int(_pitch(scale) if scale_ld is None else scale_ld), int(block_rows), 0)
-
-
-def _row_pitch(x) -> int:
-    return 0 if x is None else _pitch(x)
+    rows, cols, block_rows = int(rows), int(cols), int(block_rows)
+    at, pitch = (_addr(data), int(ld)) if ld is not None else _rows_at(data, rows, cols, 1, "data")
+    scale_rows = -(-rows // block_rows) if block_rows > 0 else 0
+    scale_at, scale_pitch = (_addr(scale), int(scale_ld)) if scale_ld is not None else \
+        _rows_at(scale, scale_rows, -(-cols // ZI_FP8_BLOCK), 1, "scale")
+    return zi_fp8_matrix(at, scale_at, rows, cols, pitch, scale_pitch, block_rows, 0)
 
 
 def make_rms_norm(x, gamma, dtype: int, eps: float, residual=None, sum=None, y=None, rstd=None) -> zi_rms_norm_args:
     """Arguments of zi_rms_norm from matrices (torch tensors or numpy arrays); None for what is not given or not wanted."""
-    rows, cols = x.shape
-    return zi_rms_norm_args(_addr(x), _addr(residual), _addr(gamma), _addr(sum), _addr(y), _addr(rstd), int(rows), int(cols),
-                            _pitch(x), _row_pitch(residual), _row_pitch(sum), _row_pitch(y), float(eps), int(dtype))
+    (rows, cols), size = x.shape, _BYTES_OF.get(dtype)
+    x, x_ld = _rows_at(x, rows, cols, size, "x")
+    residual, residual_ld = _rows_at(residual, rows, cols, size, "residual")
+    sum, sum_ld = _rows_at(sum, rows, cols, size, "sum")
+    y, y_ld = _rows_at(y, rows, cols, size, "y")
+    return zi_rms_norm_args(x, residual, _vector_at(gamma, cols, size, "gamma"), sum, y, _vector_at(rstd, rows, 4, "rstd"),
+                            int(rows), int(cols), x_ld, residual_ld, sum_ld, y_ld, float(eps), int(dtype))
 
 
 def make_rms_norm_backward(dy, h, gamma, rstd, dx, dgamma, dtype: int, dsum=None, dgamma_dtype: Optional[int] = None,
                            accumulate: bool = False) -> zi_rms_norm_backward_args:
     """Arguments of zi_rms_norm_backward, as in make_rms_norm; dgamma is of dtype where its type is not given."""
-    rows, cols = dy.shape
-    return zi_rms_norm_backward_args(_addr(dy), _addr(h), _addr(gamma), _addr(rstd), _addr(dsum), _addr(dx), _addr(dgamma),
-                                     int(rows), int(cols), _pitch(dy), _pitch(h), _row_pitch(dsum), _row_pitch(dx), int(dtype),
-                                     int(dtype if dgamma_dtype is None else dgamma_dtype), int(accumulate), 0)
+    (rows, cols), size = dy.shape, _BYTES_OF.get(dtype)
+    dgamma_dtype = dtype if dgamma_dtype is None else dgamma_dtype
+    dy, dy_ld = _rows_at(dy, rows, cols, size, "dy")
+    h, h_ld = _rows_at(h, rows, cols, size, "h")
+    dsum, dsum_ld = _rows_at(dsum, rows, cols, size, "dsum")
+    dx, dx_ld = _rows_at(dx, rows, cols, size, "dx")
+    return zi_rms_norm_backward_args(dy, h, _vector_at(gamma, cols, size, "gamma"), _vector_at(rstd, rows, 4, "rstd"), dsum, dx,
+                                     _vector_at(dgamma, cols, _BYTES_OF.get(dgamma_dtype), "dgamma"), int(rows), int(cols), dy_ld, h_ld,
+                                     dsum_ld, dx_ld, int(dtype), int(dgamma_dtype), int(accumulate), 0)
 
 
 def _ref(struct):
