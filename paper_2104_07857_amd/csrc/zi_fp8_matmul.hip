@@ -80,6 +80,15 @@ __device__ __forceinline__ void wait_and_meet()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// What the lanes of this wavefront wrote to LDS is there for each other.  The hardware does a wavefront's accesses to LDS in their order, so this is no
+// instruction: it keeps the compiler from changing that order.
+__device__ __forceinline__ void lanes_meet()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // f(number<0>()), ..., f(number<N - 1>())
 template <int I>
 using number = std::integral_constant<int, I>;
@@ -399,10 +408,12 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
                 *reinterpret_cast<u32x4*>(chunk(r, own_chunk)) = u32x4{c.w[0], c.w[1], c.w[2], c.w[3]};
             }
         }
+        lanes_meet();
         put_sums(std::true_type());
     } else {
         put_sums(std::false_type());
     }
+    lanes_meet();
     if (inside) {
         for (int turn = 0; turn < kTurns; turn += kBatch) {
             u32x4 x[kBatch];
