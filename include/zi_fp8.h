@@ -68,11 +68,13 @@ zi_status zi_fp8_quantize(const void* x, int32_t dtype, int64_t rows, int64_t co
 
 /*
  * D = A B^T + C: a is m x k, b is n x k, d and c are m x n with pitch ldd, ZI_BF16 or ZI_FP16, aligned to their
- * element; c may be NULL (nothing is added) or d (accumulation over micro-batches).  The sum over k is held in
- * fp32, c is added in fp32, and the result is rounded once.  k = 0 gives C, or zeros.
- * Pitches of operands are below 2^23.
- * The matrix cores add the products of 16 neighbouring k at a time and drop from these what lies more than about 2^-14 below the largest
- * of them: 1.5e-5 of the result (2-norm) on normal numbers, 5e-5 where one column in 64 is twenty times the others.
+ * element; c may be NULL (nothing is added) or d (accumulation over micro-batches, rounded in each).  k = 0 gives C,
+ * or zeros.  Pitches of operands are below 2^23.
+ * The matrix cores add the products of 16 neighbouring k at a time, with fewer bits than fp32 has: what lies more than
+ * about 2^-14 below the largest of the 16 is dropped, 1.5e-5 of the result (2-norm) on normal numbers, 5e-5 where one
+ * column in 64 is twenty times the others.  Their sums are added in fp32, and so is c; the result is rounded once.
+ * The order of k, and with it these roundings, depends on the sizes and on the place in D: the same call gives the same bits, but
+ * rows of A that are equal may give rows of D that differ by a rounding, and so may a row in a call with other rows.
  *   a layer y = x W^T:    a = x (block_rows 1), b = W (block_rows 128, n x k)
  *   its input's gradient: a = dy, b = W turned
  *   its weights':         a = dy turned, b = x turned (both block_rows 1)
@@ -86,8 +88,8 @@ zi_status zi_fp8_matmul(const zi_fp8_matrix* a, const zi_fp8_matrix* b, void* d,
 /*
  * Row by row, with h = x + residual rounded to dtype (h = x without a residual):
  *   rstd = 1 / sqrt(mean(h^2) + eps)      y = h * rstd * gamma
- * The mean and rstd are in fp32 (a row whose squares pass 3.4e38 in sum has rstd 0).  x, residual, sum, y: rows x cols in dtype (ZI_BF16 or ZI_FP16),
- * aligned to their element, each with its own pitch in elements.  gamma: cols in dtype.  sum (h; needs a residual), y,
+ * The mean and rstd are in fp32: a row whose squares pass 3.4e38 in sum has rstd 0; with eps 0, one of magnitudes below
+ * 2^-75 (2.6e-23) throughout has an infinite one, as a row of zeros has.  x, residual, sum, y: rows x cols in dtype (ZI_BF16 or ZI_FP16), aligned to their element, each with its own pitch in elements.  gamma: cols in dtype.  sum (h; needs a residual), y,
  * rstd (rows fp32) and y8 (block_rows 1, of the unrounded y) are outputs, NULL where they are not wanted; at least one is.
  * sum may be x or residual, y may be x, in place.  1 <= cols <= 65536.
  */

@@ -168,7 +168,7 @@ hipError_t launch_fp8_quantize(const QuantizeArgs& a, int dtype, hipStream_t s)
 // One pass: h stays in registers while its squares are summed in fp32 (lanes, then wavefronts in their order), so x and the residual are read once and
 // every output is written once.  T threads have a row, V octets each: octet v * T + t.  16 lanes have a block of 128 columns; its scale is that of the
 // unrounded y, which is rounded to 8 bits directly.  Bound by memory: 16384 x 8192 bf16 with everything 202 us (1209 MB, 6.0 TB/s, a plain copy 6.7); one
-// row of 4096 3.3 us, most of it the way to memory and back twice.
+// row of 4096 3.3 to 4.0 us, most of it the way to memory and back twice.
 template <int DT, int T, int V, Ends ENDS>
 __global__ __launch_bounds__(T) void rms_norm_kernel(const RmsNormArgs k)
 {
@@ -326,7 +326,7 @@ struct BackwardRow {
     }
 };
 
-// Bound by memory: 16384 x 4096 bf16 with dsum 91 us (537 MB, 5.9 TB/s) and 4.8 us for the shares of dgamma.
+// Bound by memory: 16384 x 4096 bf16 with dsum 92 us (537 MB, 5.8 TB/s) and 4.9 us for the shares of dgamma.
 // A workgroup goes over rows a grid apart and keeps its columns' share of dgamma in registers; the shares of all
 // workgroups are added by a second kernel in their order.  The next row's loads go out before this row's sum is known (16384 x 4096
 // with dsum 123 -> 97 us).  MEANS: rows that do not fit one workgroup's registers (is_cut) are cut, and means of whole rows come from a kernel in
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_
 }
 
 // dgamma of 16 columns: P rows of threads take every Pth share each, and are added in a fixed order.  Bound by latency: 256 shares of 4096 columns
-// 4.8 us (4.2 MB).  Eight shares' loads go out at a time (backward pass of 13683 x 152 18.4 -> 14.3, 8192 x 1024 21.3 -> 18.8).
+// 4.9 us (4.2 MB).  Eight shares' loads go out at a time (backward pass of 13683 x 152 18.4 -> 14.3, 8192 x 1024 21.3 -> 18.8).
 template <int DT, int P>
 __global__ __launch_bounds__(16 * P) void rms_norm_dgamma_kernel(const float* partials, int count, int64_t cols, void* dgamma, int accumulate)
 {
