@@ -1,4 +1,5 @@
-"""ctypes binding of libzi.so: argument marshalling only, same names as include/zi.h and include/zi_fp8.h.
+"""ctypes binding of libzi.so: argument marshalling only, same names as include/zi.h, include/zi_fp8.h and
+include/zi_epilogue.h.
 
 Every step of the path runs in the HIP kernels behind the C ABI.  There is no
 CPU fallback: if the library is missing, loading raises.
@@ -26,6 +27,13 @@ ZI_FP16 = 1
 ZI_FP32 = 2
 ZI_FP8_BLOCK = 128
 ZI_RMS_NORM_MAX_COLS = 65536
+ZI_ACT_NONE = 0
+ZI_ACT_RELU = 1
+ZI_ACT_GELU = 2
+ZI_ACT_GELU_TANH = 3
+ZI_ACT_SILU = 4
+ZI_EPILOGUE_Y8 = 1
+ZI_EPILOGUE_TURNED = 2
 ZI_MODE_ADAMW = 0
 ZI_MODE_ADAM_L2 = 1
 ZI_OPT_SKIP_KERNEL = 0
@@ -41,6 +49,7 @@ EXPORTS = [
     "zi_host_grad_norm", "zi_host_adamw_step", "zi_norm_refresh", "zi_plan_step", "zi_grad_norm_noalloc", "zi_grad_offload", "zi_grad_offload_wait", "zi_grad_offload_order", "zi_adamw_step_cpu",
     "zi_fp8_quantize", "zi_fp8_matmul", "zi_fp8_matmul_workspace_bytes", "zi_rms_norm", "zi_rms_norm_backward",
     "zi_rms_norm_workspace_bytes",
+    "zi_epilogue", "zi_epilogue_backward", "zi_epilogue_workspace_bytes", "zi_fp8_matmul_epilogue", "zi_fp8_matmul_epilogue_workspace_bytes",
 ]
 
 
@@ -108,6 +117,20 @@ class zi_rms_norm_backward_args(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("dtype", "dgamma_dtype", "accumulate", "reserved")]
 
 
+class zi_epilogue_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("bias", "residual", "z", "y", "d_offset")] + \
+               [(n, ctypes.c_uint64) for n in ("seed", "offset")] + \
+               [(n, ctypes.c_int64) for n in ("residual_ld", "z_ld", "y_ld")] + [("drop", ctypes.c_float)] + \
+               [(n, ctypes.c_int32) for n in ("activation", "dtype", "reserved")]
+
+
+class zi_epilogue_backward_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dy", "z", "dz", "dbias", "d_offset")] + \
+               [(n, ctypes.c_uint64) for n in ("seed", "offset")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "dy_ld", "z_ld", "dz_ld")] + [("drop", ctypes.c_float)] + \
+               [(n, ctypes.c_int32) for n in ("activation", "dtype", "dbias_dtype", "accumulate", "reserved")]
+
+
 _lib = None
 
 
@@ -118,10 +141,12 @@ def _not_taken(*args):
 # The calls made once per step or layer, for arguments in their usual form (csrc/zi_python.c): a status, or None for other forms.
 _call_norm = _call_norm_noalloc = _call_step = _not_taken
 _call_quantize = _call_matmul = _call_rms_norm = _call_rms_norm_backward = _not_taken
+_call_epilogue = _call_matmul_epilogue = _call_epilogue_backward = _not_taken
 
 
 def _bind_calls(L):
     global _call_norm, _call_norm_noalloc, _call_step, _call_quantize, _call_matmul, _call_rms_norm, _call_rms_norm_backward
+    global _call_epilogue, _call_matmul_epilogue, _call_epilogue_backward
     try:
         from . import _zi_call as c
     except ImportError:                # not built: everything goes through ctypes
@@ -134,6 +159,9 @@ def _bind_calls(L):
                   zi_fp8_matrix(), zi_rms_norm_args(), zi_rms_norm_backward_args()):
         _call_quantize, _call_matmul = c.fp8_quantize, c.fp8_matmul
         _call_rms_norm, _call_rms_norm_backward = c.rms_norm, c.rms_norm_backward
+    if c.bind_epilogue(address(L.zi_epilogue), address(L.zi_fp8_matmul_epilogue), address(L.zi_epilogue_backward), zi_fp8_matrix(),
+                       zi_epilogue_args(), zi_epilogue_backward_args()):
+        _call_epilogue, _call_matmul_epilogue, _call_epilogue_backward = c.epilogue, c.matmul_epilogue, c.epilogue_backward
 
 
 def lib() -> ctypes.CDLL:
@@ -220,6 +248,16 @@ def lib() -> ctypes.CDLL:
         L.zi_rms_norm_workspace_bytes.argtypes = [i64, i64]
         L.zi_rms_norm_backward.restype = ctypes.c_int
         L.zi_rms_norm_backward.argtypes = [ctypes.POINTER(zi_rms_norm_backward_args), vp, sz, vp]
+        L.zi_epilogue.restype = ctypes.c_int
+        L.zi_epilogue.argtypes = [vp, i64, i64, i64, ctypes.POINTER(zi_epilogue_args), fp8, fp8, vp]
+        L.zi_fp8_matmul_epilogue_workspace_bytes.restype = sz
+        L.zi_fp8_matmul_epilogue_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.zi_fp8_matmul_epilogue.restype = ctypes.c_int
+        L.zi_fp8_matmul_epilogue.argtypes = [fp8, fp8, ctypes.POINTER(zi_epilogue_args), fp8, fp8, vp, sz, vp]
+        L.zi_epilogue_workspace_bytes.restype = sz
+        L.zi_epilogue_workspace_bytes.argtypes = [i64, i64]
+        L.zi_epilogue_backward.restype = ctypes.c_int
+        L.zi_epilogue_backward.argtypes = [ctypes.POINTER(zi_epilogue_backward_args), fp8, fp8, vp, sz, vp]
         _lib = L
         _bind_calls(L)
     return _lib
@@ -590,4 +628,65 @@ def zi_rms_norm_backward(args: zi_rms_norm_backward_args, d_workspace=None, work
     if status is not None:
         return status if status >= 0 else _check(status)
     return _check(lib().zi_rms_norm_backward(_ref(args), _addr(d_workspace), _bytes(d_workspace, workspace_bytes),
+                                             _stream(stream)))
+
+
+# ---- what follows a product: include/zi_epilogue.h ------------------------------------------
+
+def make_epilogue(rows: int, cols: int, dtype: int, bias=None, residual=None, z=None, y=None, activation: int = ZI_ACT_NONE,
+                  drop: float = 0.0, seed: int = 0, offset: int = 0, d_offset=None) -> zi_epilogue_args:
+    """Arguments of zi_epilogue and zi_fp8_matmul_epilogue for a matrix of rows x cols, from matrices (torch tensors or numpy arrays); None for
+    what is not given or not wanted.  d_offset: an integer of 64 bits in device memory."""
+    rows, cols, size = int(rows), int(cols), _BYTES_OF.get(dtype)
+    residual, residual_ld = _rows_at(residual, rows, cols, size, "residual")
+    z, z_ld = _rows_at(z, rows, cols, size, "z")
+    y, y_ld = _rows_at(y, rows, cols, size, "y")
+    return zi_epilogue_args(_vector_at(bias, cols, size, "bias"), residual, z, y, _vector_at(d_offset, 1, 8, "d_offset"), int(seed), int(offset),
+                            residual_ld, z_ld, y_ld, float(drop), int(activation), int(dtype), 0)
+
+
+def make_epilogue_backward(dy, z, dz, dbias, dtype: int, activation: int = ZI_ACT_NONE, drop: float = 0.0, seed: int = 0, offset: int = 0,
+                           d_offset=None, dbias_dtype: Optional[int] = None, accumulate: bool = False) -> zi_epilogue_backward_args:
+    """Arguments of zi_epilogue_backward, as in make_epilogue; dbias is of dtype where its type is not given."""
+    (rows, cols), size = dy.shape, _BYTES_OF.get(dtype)
+    dbias_dtype = dtype if dbias_dtype is None else dbias_dtype
+    dy, dy_ld = _rows_at(dy, rows, cols, size, "dy")
+    z, z_ld = _rows_at(z, rows, cols, size, "z")
+    dz, dz_ld = _rows_at(dz, rows, cols, size, "dz")
+    return zi_epilogue_backward_args(dy, z, dz, _vector_at(dbias, cols, _BYTES_OF.get(dbias_dtype), "dbias"), _vector_at(d_offset, 1, 8, "d_offset"),
+                                     int(seed), int(offset), int(rows), int(cols), dy_ld, z_ld, dz_ld, float(drop), int(activation), int(dtype),
+                                     int(dbias_dtype), int(accumulate), 0)
+
+
+def zi_epilogue(x, rows: int, cols: int, ld: int, args: zi_epilogue_args, y8: Optional[zi_fp8_matrix] = None,
+                turned: Optional[zi_fp8_matrix] = None, stream=None) -> int:
+    status = _call_epilogue(x, rows, cols, ld, args, y8, turned, stream)
+    if status is not None:
+        return status if status >= 0 else _check(status)
+    return _check(lib().zi_epilogue(_addr(x), int(rows), int(cols), int(ld), _ref(args), _ref(y8), _ref(turned), _stream(stream)))
+
+
+def zi_fp8_matmul_epilogue_workspace_bytes(m: int, n: int, k: int, outputs8: int = 0) -> int:
+    return int(lib().zi_fp8_matmul_epilogue_workspace_bytes(int(m), int(n), int(k), int(outputs8)))
+
+
+def zi_fp8_matmul_epilogue(a: zi_fp8_matrix, b: zi_fp8_matrix, args: zi_epilogue_args, y8: Optional[zi_fp8_matrix] = None,
+                           turned: Optional[zi_fp8_matrix] = None, d_workspace=None, workspace_bytes: Optional[int] = None, stream=None) -> int:
+    status = _call_matmul_epilogue(a, b, args, y8, turned, d_workspace, workspace_bytes, stream)
+    if status is not None:
+        return status if status >= 0 else _check(status)
+    return _check(lib().zi_fp8_matmul_epilogue(_ref(a), _ref(b), _ref(args), _ref(y8), _ref(turned), _addr(d_workspace),
+                                               _bytes(d_workspace, workspace_bytes), _stream(stream)))
+
+
+def zi_epilogue_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().zi_epilogue_workspace_bytes(int(rows), int(cols)))
+
+
+def zi_epilogue_backward(args: zi_epilogue_backward_args, dz8: Optional[zi_fp8_matrix] = None, turned: Optional[zi_fp8_matrix] = None,
+                         d_workspace=None, workspace_bytes: Optional[int] = None, stream=None) -> int:
+    status = _call_epilogue_backward(args, dz8, turned, d_workspace, workspace_bytes, stream)
+    if status is not None:
+        return status if status >= 0 else _check(status)
+    return _check(lib().zi_epilogue_backward(_ref(args), _ref(dz8), _ref(turned), _addr(d_workspace), _bytes(d_workspace, workspace_bytes),
                                              _stream(stream)))

@@ -15,7 +15,8 @@ LIB_PATH = os.path.join(HERE, "libzi.so")
 # (it uses more than the limited API, so its name has this interpreter's version in it)
 CALL_PATH = os.path.join(HERE, "_zi_call" + importlib.machinery.EXTENSION_SUFFIXES[0])
 SOURCES = ["zi_kernels.hip", "zi_api.hip", "zi_plan.hip", "zi_engine.hip", "zi_offload.hip", "zi_probe.hip",
-           "zi_fp8_api.hip", "zi_fp8_rows.hip", "zi_fp8_matmul.hip"]
+           "zi_fp8_api.hip", "zi_fp8_rows.hip", "zi_fp8_matmul.hip",
+           "zi_epilogue_api.hip", "zi_epilogue.hip", "zi_fp8_matmul_epilogue.hip"]
 
 # -ffp-contract=off: the only fused multiply-adds are the ones the kernels write as fma.
 # Packed fp32 instructions are switched off for the device code.
@@ -49,7 +50,7 @@ def needs_build() -> bool:
         return True
     t = min(os.path.getmtime(f) for f in built)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + \
-           [os.path.join(ROOT, "include", f) for f in ("zi.h", "zi_fp8.h", "zi_probe.h")]
+           [os.path.join(ROOT, "include", f) for f in ("zi.h", "zi_fp8.h", "zi_epilogue.h", "zi_probe.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

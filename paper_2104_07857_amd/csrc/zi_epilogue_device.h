@@ -1,0 +1,132 @@
+// Activations, their derivatives and dropout's generator, as the kernels of the epilogues use them (include/zi_epilogue.h has the formulas).
+#pragma once
+
+#include "zi_epilogue_internal.h"
+#include "zi_fp8_device.h"
+
+namespace zi {
+
+// ---- activations ----------------------------------------------------------------------------------------------
+
+// exp and 1 / x are the hardware's (one step off at most; results below 2^-126 are zero): what is made of them is rounded to 16 or 8 bits.
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float inverse(float x) { return __builtin_amdgcn_rcpf(x); }
+constexpr float kLog2E = 1.44269504f;
+
+// 1 / (1 + exp(-z)) for z = -x / log2 e
+__device__ __forceinline__ float sigmoid_of_exponent(float x) { return inverse(1.0f + exp2_of(x)); }
+
+// Phi(-t) = exp(-t^2 / 2) R(t) for t >= 0, where R falls slowly from 1/2: a polynomial in 1 / (1 + 0.3 t), fitted to the smallest largest relative error on [0, 14.5]
+// (6e-8; 4.2e-7 as it is computed here).  `e` is exp(-t^2 / 2), which the derivative needs too.
+__device__ __forceinline__ float normal_cdf(float z, float& e)
+{
+    const float t = __builtin_fabsf(z), w = inverse(__builtin_fmaf(0.3f, t, 1.0f));
+    float r = 0.038407549262046814f;
+    r = __builtin_fmaf(r, w, -0.16930820047855377f);
+    r = __builtin_fmaf(r, w, 0.2289532572031021f);
+    r = __builtin_fmaf(r, w, -0.07684128731489182f);
+    r = __builtin_fmaf(r, w, 0.1427663415670395f);
+    r = __builtin_fmaf(r, w, 0.09458543360233307f);
+    r = __builtin_fmaf(r, w, 0.12194536626338959f);
+    r = __builtin_fmaf(r, w, 0.11948419362306595f);
+    r = __builtin_fmaf(r, w, 7.373110292974161e-06f);
+    e = exp2_of(z * z * (-0.5f * kLog2E));
+    r *= e;
+    return z < 0.0f ? r : 1.0f - r;
+}
+
+constexpr float kTanh = 1.5957691216f, kTanhCube = 0.0713548163f;        // 2 sqrt(2 / pi), and that times 0.044715
+
+template <int ACT>
+__device__ __forceinline__ float activated(float z)
+{
+    if constexpr (ACT == ZI_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    else if constexpr (ACT == ZI_ACT_GELU) {
+        float e;
+        return z * normal_cdf(z, e);
+    } else if constexpr (ACT == ZI_ACT_GELU_TANH) {
+        return z * sigmoid_of_exponent(z * __builtin_fmaf(z * z, -kLog2E * kTanhCube, -kLog2E * kTanh));
+    } else if constexpr (ACT == ZI_ACT_SILU) return z * sigmoid_of_exponent(-kLog2E * z);
+    else return z;
+}
+// dy times the derivative.  (Where a sigmoid s is 0 or 1, s - s^2 is 0, which its large factors are multiplied to one after the other.)
+template <int ACT>
+__device__ __forceinline__ float with_derivative(float dy, float z)
+{
+    if constexpr (ACT == ZI_ACT_RELU) return z <= 0.0f ? 0.0f : dy;
+    else if constexpr (ACT == ZI_ACT_GELU) {
+        float e;
+        const float phi = normal_cdf(z, e);
+        return dy * __builtin_fmaf(z * e, 0.398942280f, phi);
+    } else if constexpr (ACT == ZI_ACT_GELU_TANH) {
+        const float z2 = __builtin_fminf(z * z, 256.0f);                    // (beyond 16, s - s^2 is 0)
+        const float s = sigmoid_of_exponent(z * __builtin_fmaf(z * z, -kLog2E * kTanhCube, -kLog2E * kTanh));
+        return dy * __builtin_fmaf(__builtin_fmaf(-s, s, s) * z, __builtin_fmaf(z2, 3.0f * kTanhCube, kTanh), s);
+    } else if constexpr (ACT == ZI_ACT_SILU) {
+        const float s = sigmoid_of_exponent(-kLog2E * z);
+        return dy * __builtin_fmaf(__builtin_fmaf(-s, s, s), z, s);
+    } else return dy;
+}
+// f(activation as a type), for an activation that is the same in all lanes.
+template <typename F>
+__device__ __forceinline__ void with_activation(int activation, const F& f)
+{
+    switch (activation) {
+    case ZI_ACT_RELU: return f(std::integral_constant<int, ZI_ACT_RELU>());
+    case ZI_ACT_GELU: return f(std::integral_constant<int, ZI_ACT_GELU>());
+    case ZI_ACT_GELU_TANH: return f(std::integral_constant<int, ZI_ACT_GELU_TANH>());
+    case ZI_ACT_SILU: return f(std::integral_constant<int, ZI_ACT_SILU>());
+    }
+}
+__device__ __forceinline__ void activate(float (&x)[8], int activation)
+{
+    with_activation(activation, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = activated<decltype(act)::value>(x[j]);
+    });
+}
+
+// ---- dropout --------------------------------------------------------------------------------------------------
+
+// Philox4x32-10: ten rounds, of two 32 x 32 -> 64 multiplications each, on a counter of four words.  One call is eight columns' numbers.
+struct Dropout {
+    uint32_t key0, key1, offset0, offset1, threshold;
+    float scale;
+
+    __device__ __forceinline__ explicit Dropout(const DropoutArgs& a) : key0((uint32_t)a.seed), key1((uint32_t)(a.seed >> 32)), threshold(a.threshold), scale(a.scale)
+    {
+        const uint64_t offset = a.offset + (a.threshold && a.d_offset ? *a.d_offset : 0);
+        offset0 = (uint32_t)offset;
+        offset1 = (uint32_t)(offset >> 32);
+    }
+    __device__ __forceinline__ u32x4 numbers(uint32_t octet, uint32_t row) const
+    {
+        uint32_t x0 = octet, x1 = row, x2 = offset0, x3 = offset1, k0 = key0, k1 = key1;
+#pragma unroll
+        for (int i = 0; i < 10; ++i) {
+            const uint64_t a = (uint64_t)x0 * 0xD2511F53u, b = (uint64_t)x2 * 0xCD9E8D57u;
+            x0 = (uint32_t)(b >> 32) ^ x1 ^ k0;
+            x1 = (uint32_t)b;
+            x2 = (uint32_t)(a >> 32) ^ x3 ^ k1;
+            x3 = (uint32_t)a;
+            k0 += 0x9E3779B9u;
+            k1 += 0xBB67AE85u;
+        }
+        return u32x4{x0, x1, x2, x3};
+    }
+    __device__ __forceinline__ bool active() const { return threshold != 0; }
+    __device__ __forceinline__ static bool is_kept(const u32x4& w, int j, uint32_t threshold)
+    {
+        return (uint16_t)(w[j / 2] >> (16 * (j % 2))) >= (uint16_t)threshold;
+    }
+    // Eight columns of a row, from 8 * octet on.
+    __device__ __forceinline__ void apply(float (&x)[8], uint32_t octet, uint32_t row) const
+    {
+        if (!active()) return;
+        const u32x4 w = numbers(octet, row);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = is_kept(w, j, threshold) ? x[j] * scale : 0.0f;
+    }
+};
+
+}  // namespace zi

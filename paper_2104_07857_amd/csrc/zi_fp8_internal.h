@@ -36,6 +36,9 @@ size_t rms_norm_workspace_floats(int64_t rows, int64_t cols);     // of the back
 bool rms_norm_needs_means(int64_t cols);                          // it needs them without dgamma too
 hipError_t launch_rms_norm_backward(const zi_rms_norm_backward_args& a, float* workspace, hipStream_t s);
 
+// out (cols elements; with accumulate added to) of `count` rows of cols sums, added in a fixed order.
+hipError_t launch_column_sums(const float* partials, int count, int64_t cols, void* out, int dtype, int accumulate, hipStream_t s);
+
 struct MatmulArgs {
     const uint8_t* a;
     const uint8_t* b;

@@ -2,37 +2,15 @@
 // All are bound by memory; see include/zi_fp8.h for the formulas.  Compile with -ffp-contract=off.
 #include <hip/hip_runtime.h>
 
-#include "zi_fp8_device.h"
-#include "zi_fp8_internal.h"
+#include "zi_fp8_tile.h"
 
 namespace zi {
 
 // ---- quantisation ---------------------------------------------------------------------------------------------
 
-// A workgroup takes a tile of 128 x 128, which holds whole blocks of every kind, so x is read once whatever is wanted.
-// A thread has 8 x 8 elements in registers; 16 threads (a row of lanes) have a tile's row, so the largest of a row's
-// block comes from its lanes and that of a column's block from the thread's own rows, two steps over lanes and four
-// wavefronts.  The transposed numbers pass through LDS, which makes rows of 128 bytes of them.  16384 x 4096 fp32 in squares, both 73 us (403 MB, 5.5 TB/s);
-// 8191 x 8192 bf16, blocks of rows, both 55 us (269 MB, 4.9 TB/s, with 6 MB more of scales that were written in pieces); one row of 1000 3.7 us.
-constexpr int kTile = kFp8Block;
-
-// Each XCD has a run of tiles that goes down four rows of tiles before the next column, so that its L2 joins the bytes that neighbours write
-// to a line of scales, and begins at another eighth of its run, so that all of them do not go through the same memory channels at a time.  us, row by
-// row / so / without the other starts / in eight rows: 8192 x 8192 fp32, blocks of rows, both 81.3 / 76.4 / 85.6 / 80.8, 16384 x 8192 bf16 111.9 /
-// 106.4 / 133 / 111, 16384 x 4096 fp32 in squares 73.6 / 73.3 / 87.1 / 76.7, 300 x 30000 bf16 12.1 / 11.2 / 11.1 / 11.2.
-constexpr uint32_t kTileRows = 4, kXcds = 8;
-__device__ __forceinline__ void place_of_tile(uint32_t b, uint32_t count, uint32_t across, int64_t& row, int64_t& col)
-{
-    const uint32_t xcd = b % kXcds, least = count / kXcds, more = count % kXcds, mine = least + (xcd < more);
-    uint32_t i = b / kXcds + (uint32_t)((uint64_t)mine * xcd / kXcds);
-    if (i >= mine) i -= mine;
-    const uint32_t t = xcd * least + (xcd < more ? xcd : more) + i;
-    const uint32_t band = t / (kTileRows * across), in = t - band * kTileRows * across, under = count / across - band * kTileRows;
-    const uint32_t height = under < kTileRows ? under : kTileRows;
-    row = band * kTileRows + in % height;
-    col = in / height;
-}
-
+// A workgroup takes a tile of 128 x 128, which holds whole blocks of every kind, so x is read once whatever is wanted; a thread has 8 x 8 elements in
+// registers.  16384 x 4096 fp32 in squares, both 73 us (403 MB, 5.5 TB/s); 8191 x 8192 bf16, blocks of rows, both 55 us (269 MB, 4.9 TB/s, with 6 MB
+// more of scales that were written in pieces); one row of 1000 3.7 us.
 // LARGE: the outputs do not stay in the memory-side cache for whoever reads them next.  Their stores pass it by then.  us, ordinary / so: 32768 x 8192
 // fp32 in squares, both 316 / 287, 16384 x 8192 bf16 114 / 102; but quantisation and product of 4096 x 4096 (x 4096) 70 / 75.
 // Large outputs of fp32 keep to two workgroups on a compute unit, three where registers allow them: 16384 x 4096 in squares 72.8 / 77.1, 32768 x 8192 280 /
@@ -41,17 +19,10 @@ constexpr int64_t kLargeBytes = (int64_t)96 << 20;
 template <int DT, bool LARGE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, LARGE && DT == ZI_FP32 ? 2 : 8))) void fp8_quantize_kernel(const QuantizeArgs a)
 {
-    __shared__ uint32_t s_col[4][kTile / 8 * Octet<DT>::kWords];
-    __shared__ uint32_t s_all[4];
-    __shared__ __align__(16) uint8_t s_turned[kTile * kTile];
-
-    const int t = threadIdx.x, o = t & 15, g = t >> 4, wave = t >> 6;
+    __shared__ TileSpace<DT> s_space;
+    const int t = threadIdx.x, o = t & 15, g = t >> 4;
     int64_t tile_row, tile_col;
     place_of_tile(blockIdx.x, gridDim.x, a.tiles_across, tile_row, tile_col);
-    const auto put = [](auto x, auto* at) {
-        if constexpr (LARGE) __builtin_nontemporal_store(x, at);
-        else *at = x;
-    };
     const int64_t row0 = tile_row * kTile + g * 8, col0 = tile_col * kTile + o * 8;
     const int64_t left = a.cols - col0;
     const int in_row = left >= 8 ? 8 : left > 0 ? (int)left : 0, in_row_or_less = left >= 8 ? 8 : (int)left;
@@ -73,79 +44,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, LARGE &&
             for (int i = 0; i < 8; ++i) x[i].template settle<Ends::kMoved>(in_row_or_less);
         }
     }
-
-    constexpr int kWords = Octet<DT>::kWords;
-    uint32_t row_most[8], col_most[kWords], most;
-    const auto look = [&](auto finite) {
-        most = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint32_t m[kWords];
-#pragma unroll
-            for (int w = 0; w < kWords; ++w) {
-                m[w] = magnitudes<DT, decltype(finite)::value>(x[i].w[w]);
-                col_most[w] = i == 0 ? m[w] : max_of_words<DT>(col_most[w], m[w]);
-            }
-#pragma unroll
-            for (int w = 1; w < kWords; ++w) m[0] = max_of_words<DT>(m[0], m[w]);
-            row_most[i] = larger<DT>(m[0]);
-            most = max_of(most, row_most[i]);
-        }
-    };
-    look(std::false_type());
-    if (most >= kInfinity<DT>) look(std::true_type());
-    const bool square = a.out_square || a.turned_square, columns = a.turned && !a.turned_square;
-    if (square) {
-        most = max_of_rows<ZI_FP32>(max_16(most));
-        if ((t & 63) == 0) s_all[wave] = most;
-    }
-    if (columns) {
-#pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-            const uint32_t m = max_of_rows<DT>(col_most[w]);
-            if ((t & 63) < 16) s_col[wave][o * kWords + w] = m;
-        }
-    }
-    if (square || columns) __syncthreads();
-    uint32_t all = 127;
-    if (square) all = scale_byte(as_fp32<DT>(max_of(max_of(s_all[0], s_all[1]), max_of(s_all[2], s_all[3]))));
-
-    if (a.out) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t byte = a.out_square ? all : scale_byte(as_fp32<DT>(max_16(row_most[i])));
-            if (row0 + i >= a.rows || in_row == 0) continue;
-            put(eight_e4m3<DT>(x[i], scale_of(byte)), reinterpret_cast<u32x2*>(a.out + (row0 + i) * a.out_ld + col0));
-            if (!a.out_square && o == 0) a.out_scale[(row0 + i) * a.out_scale_ld + tile_col] = (uint8_t)byte;
-        }
-        if (a.out_square && t == 0) a.out_scale[tile_row * a.out_scale_ld + tile_col] = (uint8_t)all;
-    }
-    if (!a.turned) return;
-
-    // A column's 128 numbers are eight chunks of 16 bytes; chunk p of column c lies at p ^ (c / 8 % 8), so that the 16
-    // threads that write one row's octets reach different banks.
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int c = o * 8 + j;
-        uint32_t byte = all;
-        if (!a.turned_square) {
-            const int w = c * kWords / 8;
-            const uint32_t m = max_of_words<DT>(max_of_words<DT>(s_col[0][w], s_col[1][w]), max_of_words<DT>(s_col[2][w], s_col[3][w]));
-            byte = scale_byte(as_fp32<DT>(DT == ZI_FP32 ? m : c % 2 ? m >> 16 : m & 0xFFFFu));
-        }
-        *reinterpret_cast<u32x2*>(s_turned + c * kTile + (((g >> 1) ^ (o & 7)) << 4) + (g & 1) * 8) = eight_e4m3_down<DT>(x, j, scale_of(byte));
-        if (!a.turned_square && g == 0 && j < in_row) a.turned_scale[(col0 + j) * a.turned_scale_ld + tile_row] = (uint8_t)byte;
-    }
-    if (a.turned_square && t == 0) a.turned_scale[tile_col * a.turned_scale_ld + tile_row] = (uint8_t)all;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = i * 32 + (t >> 3), part = t & 7;
-        const int64_t col = tile_col * kTile + c, row = tile_row * kTile + part * 16;
-        if (col >= a.cols || row >= a.rows) continue;
-        put(*reinterpret_cast<const u32x4*>(s_turned + c * kTile + ((part ^ ((c >> 3) & 7)) << 4)),
-            reinterpret_cast<u32x4*>(a.turned + col * a.turned_ld + row));
-    }
+    quantize_tile<DT, LARGE>(a, x, tile_row, tile_col, s_space);
 }
 
 template <int DT>
@@ -399,7 +298,7 @@ __global__ __launch_bounds__(1024) void rms_norm_means_kernel(const zi_rms_norm_
     }
 }
 
-// dgamma of 16 columns: P rows of threads take every Pth share each, and are added in a fixed order.  Bound by latency: 256 shares of 4096 columns
+// dgamma (or other sums over rows) of 16 columns: P rows of threads take every Pth share each, and are added in a fixed order.  Bound by latency: 256 shares of 4096 columns
 // 4.9 us (4.2 MB).  Eight shares' loads go out at a time (backward pass of 13683 x 152 18.4 -> 14.3, 8192 x 1024 21.3 -> 18.8).
 template <int DT, int P>
 __global__ __launch_bounds__(16 * P) void rms_norm_dgamma_kernel(const float* partials, int count, int64_t cols, void* dgamma, int accumulate)
@@ -544,11 +443,18 @@ static int64_t backward_groups(int64_t rows, int64_t cols)
 }
 
 template <int DT>
-static void launch_dgamma(const zi_rms_norm_backward_args& a, const float* partials, int groups, hipStream_t s)
+static void launch_sums(const float* partials, int count, int64_t cols, void* out, int accumulate, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.cols + 15) / 16));
-    if (groups <= 64) hipLaunchKernelGGL((rms_norm_dgamma_kernel<DT, 16>), grid, dim3(256), 0, s, partials, groups, a.cols, a.dgamma, a.accumulate);
-    else hipLaunchKernelGGL((rms_norm_dgamma_kernel<DT, 64>), grid, dim3(1024), 0, s, partials, groups, a.cols, a.dgamma, a.accumulate);
+    const dim3 grid((unsigned)((cols + 15) / 16));
+    if (count <= 64) hipLaunchKernelGGL((rms_norm_dgamma_kernel<DT, 16>), grid, dim3(256), 0, s, partials, count, cols, out, accumulate);
+    else hipLaunchKernelGGL((rms_norm_dgamma_kernel<DT, 64>), grid, dim3(1024), 0, s, partials, count, cols, out, accumulate);
+}
+hipError_t launch_column_sums(const float* partials, int count, int64_t cols, void* out, int dtype, int accumulate, hipStream_t s)
+{
+    if (dtype == ZI_BF16) launch_sums<ZI_BF16>(partials, count, cols, out, accumulate, s);
+    else if (dtype == ZI_FP16) launch_sums<ZI_FP16>(partials, count, cols, out, accumulate, s);
+    else launch_sums<ZI_FP32>(partials, count, cols, out, accumulate, s);
+    return hipGetLastError();
 }
 
 size_t rms_norm_workspace_floats(int64_t rows, int64_t cols)
@@ -567,11 +473,7 @@ hipError_t launch_rms_norm_backward(const zi_rms_norm_backward_args& a, float* p
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (!a.dgamma) return hipSuccess;
-    if (a.dgamma_dtype == ZI_BF16) launch_dgamma<ZI_BF16>(a, partials, (int)groups, s);
-    else if (a.dgamma_dtype == ZI_FP16) launch_dgamma<ZI_FP16>(a, partials, (int)groups, s);
-    else launch_dgamma<ZI_FP32>(a, partials, (int)groups, s);
-    return hipGetLastError();
+    return a.dgamma ? launch_column_sums(partials, (int)groups, a.cols, a.dgamma, a.dgamma_dtype, a.accumulate, s) : hipSuccess;
 }
 
 }  // namespace zi

@@ -1,5 +1,5 @@
 /* The calls that a training loop makes once per step or per layer, for Python: the arguments of zi_grad_norm, zi_grad_norm_noalloc,
- * zi_adamw_step and the operators of zi_fp8.h are taken out of their objects here.  On a short tensor such a call is bound by the host, and ctypes
+ * zi_adamw_step and the operators of zi_fp8.h and zi_epilogue.h are taken out of their objects here.  On a short tensor such a call is bound by the host, and ctypes
  * spends on its arguments what the library spends on the launch: norm and step on 1003 elements 9.5 us through ctypes, 7.0
  * without any binding.
  *
@@ -13,6 +13,7 @@
 #include <stdint.h>
 
 #include "zi.h"
+#include "zi_epilogue.h"
 #include "zi_fp8.h"
 
 static zi_status (*grad_norm)(const zi_tensor*, int32_t, zi_lp_dtype, float, zi_norm_result*, void*, size_t, void*);
@@ -26,9 +27,16 @@ static quantize_type* quantize;
 static matmul_type* matmul;
 static rms_norm_type* rms_norm;
 static rms_norm_backward_type* rms_norm_backward;
+typedef zi_status epilogue_type(const void*, int64_t, int64_t, int64_t, const zi_epilogue_args*, const zi_fp8_matrix*, const zi_fp8_matrix*, void*);
+typedef zi_status matmul_epilogue_type(const zi_fp8_matrix*, const zi_fp8_matrix*, const zi_epilogue_args*, const zi_fp8_matrix*, const zi_fp8_matrix*, void*, size_t, void*);
+typedef zi_status epilogue_backward_type(const zi_epilogue_backward_args*, const zi_fp8_matrix*, const zi_fp8_matrix*, void*, size_t, void*);
+static epilogue_type* epilogue;
+static matmul_epilogue_type* matmul_epilogue;
+static epilogue_backward_type* epilogue_backward;
 static PyObject *s_data_ptr, *s_cuda_stream, *s_numel, *s_element_size;
 /* how ctypes describes the structures */
-static char tensor_format[256], config_format[256], matrix_format[256], norm_format[512], backward_format[512];
+static char tensor_format[256], config_format[256], matrix_format[256], norm_format[512], backward_format[512], epilogue_format[512], epilogue_backward_format[512],
+    epilogue_matrix_format[256];
 
 /* 1 and the value, or 0 without an error set. */
 static int as_int(PyObject* x, long long lo, long long hi, long long* out)
@@ -292,6 +300,100 @@ static PyObject* bind_fp8(PyObject* self, PyObject* const* a, Py_ssize_t n_args)
     Py_RETURN_TRUE;
 }
 
+/* Structures or None, as struct_of takes each of them: all or none. */
+static int structs_of(PyObject* const* x, const char* const* format, Py_buffer* view, int count)
+{
+    for (int i = 0; i < count; ++i) {
+        if (struct_of(x[i], format[i], &view[i])) continue;
+        while (i-- > 0) PyBuffer_Release(&view[i]);
+        return 0;
+    }
+    return 1;
+}
+static void release(Py_buffer* view, int count)
+{
+    for (int i = 0; i < count; ++i) PyBuffer_Release(&view[i]);
+}
+
+/* x, rows, cols, ld, args, y8, turned, stream */
+static PyObject* call_epilogue(PyObject* self, PyObject* const* a, Py_ssize_t n_args)
+{
+    const char* const formats[3] = {epilogue_format, epilogue_matrix_format, epilogue_matrix_format};
+    long long rows, cols, ld;
+    void *x, *stream;
+    Py_buffer v[3];
+    zi_status st;
+    if (n_args != 8 || !as_pointer(a[0], s_data_ptr, NULL, &x) || !as_int(a[1], INT64_MIN, INT64_MAX, &rows) || !as_int(a[2], INT64_MIN, INT64_MAX, &cols) ||
+        !as_int(a[3], INT64_MIN, INT64_MAX, &ld) || !as_pointer(a[7], NULL, s_cuda_stream, &stream) || !structs_of(a + 4, formats, v, 3))
+        Py_RETURN_NONE;
+    Py_BEGIN_ALLOW_THREADS
+    st = epilogue(x, rows, cols, ld, (const zi_epilogue_args*)v[0].buf, (const zi_fp8_matrix*)v[1].buf, (const zi_fp8_matrix*)v[2].buf, stream);
+    Py_END_ALLOW_THREADS
+    release(v, 3);
+    return PyLong_FromLong((long)st);
+}
+
+/* a, b, args, y8, turned, workspace, its bytes, stream */
+static PyObject* call_matmul_epilogue(PyObject* self, PyObject* const* a, Py_ssize_t n_args)
+{
+    const char* const formats[5] = {epilogue_matrix_format, epilogue_matrix_format, epilogue_format, epilogue_matrix_format, epilogue_matrix_format};
+    long long bytes;
+    void *ws, *stream;
+    Py_buffer v[5];
+    zi_status st;
+    if (n_args != 8 || !as_pointer(a[5], s_data_ptr, NULL, &ws) || !bytes_of(a[5], a[6], &bytes) || !as_pointer(a[7], NULL, s_cuda_stream, &stream) ||
+        !structs_of(a, formats, v, 5))
+        Py_RETURN_NONE;
+    Py_BEGIN_ALLOW_THREADS
+    st = matmul_epilogue((const zi_fp8_matrix*)v[0].buf, (const zi_fp8_matrix*)v[1].buf, (const zi_epilogue_args*)v[2].buf, (const zi_fp8_matrix*)v[3].buf,
+                         (const zi_fp8_matrix*)v[4].buf, ws, (size_t)bytes, stream);
+    Py_END_ALLOW_THREADS
+    release(v, 5);
+    return PyLong_FromLong((long)st);
+}
+
+/* args, dz8, turned, workspace, its bytes, stream */
+static PyObject* call_epilogue_backward(PyObject* self, PyObject* const* a, Py_ssize_t n_args)
+{
+    const char* const formats[3] = {epilogue_backward_format, epilogue_matrix_format, epilogue_matrix_format};
+    long long bytes;
+    void *ws, *stream;
+    Py_buffer v[3];
+    zi_status st;
+    if (n_args != 6 || !as_pointer(a[3], s_data_ptr, NULL, &ws) || !bytes_of(a[3], a[4], &bytes) || !as_pointer(a[5], NULL, s_cuda_stream, &stream) ||
+        !structs_of(a, formats, v, 3))
+        Py_RETURN_NONE;
+    Py_BEGIN_ALLOW_THREADS
+    st = epilogue_backward((const zi_epilogue_backward_args*)v[0].buf, (const zi_fp8_matrix*)v[1].buf, (const zi_fp8_matrix*)v[2].buf, ws, (size_t)bytes, stream);
+    Py_END_ALLOW_THREADS
+    release(v, 3);
+    return PyLong_FromLong((long)st);
+}
+
+/* bind_epilogue(addresses of zi_epilogue, zi_fp8_matmul_epilogue, zi_epilogue_backward, a zi_fp8_matrix, a zi_epilogue_args, a zi_epilogue_backward_args): as
+ * bind. */
+static PyObject* bind_epilogue(PyObject* self, PyObject* const* a, Py_ssize_t n_args)
+{
+    void* f[3];
+    Py_buffer view;
+    char* const formats[3] = {epilogue_matrix_format, epilogue_format, epilogue_backward_format};
+    const size_t room[3] = {sizeof epilogue_matrix_format, sizeof epilogue_format, sizeof epilogue_backward_format};
+    const Py_ssize_t sizes[3] = {(Py_ssize_t)sizeof(zi_fp8_matrix), (Py_ssize_t)sizeof(zi_epilogue_args), (Py_ssize_t)sizeof(zi_epilogue_backward_args)};
+    int ok = n_args == 6;
+    for (int i = 0; ok && i < 3; ++i) ok = as_pointer(a[i], s_data_ptr, NULL, &f[i]) && f[i];
+    for (int i = 0; ok && i < 3; ++i) {
+        if (PyObject_GetBuffer(a[3 + i], &view, PyBUF_FORMAT | PyBUF_ND) != 0) return NULL;
+        ok = view.itemsize == sizes[i] && view.format && strlen(view.format) < room[i];
+        if (ok) strcpy(formats[i], view.format);
+        PyBuffer_Release(&view);
+    }
+    if (!ok) Py_RETURN_FALSE;
+    epilogue = (epilogue_type*)f[0];
+    matmul_epilogue = (matmul_epilogue_type*)f[1];
+    epilogue_backward = (epilogue_backward_type*)f[2];
+    Py_RETURN_TRUE;
+}
+
 /* bind(address of zi_grad_norm, of zi_grad_norm_noalloc, of zi_adamw_step, a zi_tensor, a zi_adamw_config): True if these
  * are the structures that this module was compiled with. */
 static PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n_args)
@@ -325,6 +427,10 @@ static PyMethodDef methods[] = {
     {"fp8_matmul", (PyCFunction)(void (*)(void))call_fp8_matmul, METH_FASTCALL, NULL},
     {"rms_norm", (PyCFunction)(void (*)(void))call_rms_norm, METH_FASTCALL, NULL},
     {"rms_norm_backward", (PyCFunction)(void (*)(void))call_rms_norm_backward, METH_FASTCALL, NULL},
+    {"bind_epilogue", (PyCFunction)(void (*)(void))bind_epilogue, METH_FASTCALL, NULL},
+    {"epilogue", (PyCFunction)(void (*)(void))call_epilogue, METH_FASTCALL, NULL},
+    {"matmul_epilogue", (PyCFunction)(void (*)(void))call_matmul_epilogue, METH_FASTCALL, NULL},
+    {"epilogue_backward", (PyCFunction)(void (*)(void))call_epilogue_backward, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_zi_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
