@@ -1,6 +1,7 @@
 """Builds libzi.so (HIP kernels + C ABI) for gfx950 with hipcc and the module _zi_call (argument marshalling) with gcc, in-tree."""
 from __future__ import annotations
 
+import concurrent.futures
 import importlib.machinery
 import os
 import shutil
@@ -84,6 +85,17 @@ def build_call() -> str | None:
     return CALL_PATH
 
 
+def _run_hipcc(cmd):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    noise = "packed-fp32-ops' is not a recognized feature"
+    err = "\n".join(l for l in r.stderr.splitlines() if noise not in l)
+    if r.returncode != 0:
+        sys.stderr.write(err + "\n")
+        raise RuntimeError("hipcc failed: " + " ".join(cmd))
+    if err.strip():
+        sys.stderr.write(err + "\n")
+
+
 def build(force: bool = True, extra_flags=(), out: str | None = None) -> str:
     out = out or LIB_PATH
     if not force and out == LIB_PATH and not needs_build():
@@ -96,16 +108,16 @@ def build(force: bool = True, extra_flags=(), out: str | None = None) -> str:
         subprocess.run(["g++", *HOST_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", os.path.join(CSRC, src),
                         "-o", obj], check=True)
         objs.append(obj)
-    cmd = [hipcc(), *HIPCC_FLAGS, *extra_flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-o", out, *[os.path.join(CSRC, s) for s in SOURCES], *["-Wl," + o for o in objs], "-pthread"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    noise = "packed-fp32-ops' is not a recognized feature"
-    err = "\n".join(l for l in r.stderr.splitlines() if noise not in l)
-    if r.returncode != 0:
-        sys.stderr.write(err + "\n")
-        raise RuntimeError("hipcc failed: " + " ".join(cmd))
-    if err.strip():
-        sys.stderr.write(err + "\n")
+    # A source a process, as many as there are CPUs (16 at most); each leaves an object of its own next to the library that is made of them.
+    flags = [*HIPCC_FLAGS, *extra_flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    stem = os.path.splitext(out)[0]
+    hip_objs = [f"{stem}_{os.path.splitext(src)[0]}.o" for src in SOURCES]
+    compiles = [[hipcc(), *(f for f in flags if f != "-shared"), "-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, hip_objs)]
+    with concurrent.futures.ThreadPoolExecutor(max(1, min(16, os.cpu_count() or 1))) as pool:
+        list(pool.map(_run_hipcc, compiles))
+    _run_hipcc([hipcc(), "--offload-arch=gfx950", "-shared", "-o", out, *hip_objs, *objs, "-pthread"])
+    for obj in hip_objs:
+        os.remove(obj)
     return out
 
 

@@ -1,5 +1,5 @@
 // Kernels of what follows a product, by itself, and of its gradients (include/zi_epilogue.h).  All are bound by memory, with dropout or an activation close to what the vector units do
-// meanwhile.  Compile with -ffp-contract=off.
+// meanwhile, so every kernel is made for one activation (but those of sums and of rows of less than eight).  Compile with -ffp-contract=off.
 #include <hip/hip_runtime.h>
 
 #include "zi_epilogue_device.h"
@@ -7,26 +7,34 @@
 
 namespace zi {
 
-// ---- forward --------------------------------------------------------------------------------------------------
+// ---- octets ---------------------------------------------------------------------------------------------------
+
+// `valid` columns of an octet, of which there are eight or (ENDS kWhole) none.
+template <Ends ENDS, typename T>
+__device__ __forceinline__ void put_octet(const T& x, void* base, int64_t at, int left, bool stream)
+{
+    if constexpr (ENDS == Ends::kWhole) {
+        if (left <= 0) return;
+        left = 8;
+    }
+    if (left <= 0) return;
+    if (stream) x.template store<true>(base, at, left);
+    else x.store(base, at, left);
+}
 
 // An octet's x (16 bits, or sums of a product's parts in their order) and how it becomes y.
-template <int DT, bool SUMS, Ends ENDS>
+template <int DT, int ACT, bool SUMS, Ends ENDS>
 struct EpilogueOctet {
     Octet<SUMS ? ZI_FP32 : DT> x;
     Octet<DT> residual;
 
-    __device__ __forceinline__ void clear()
-    {
-        x.clear();
-        residual.clear();
-    }
     __device__ __forceinline__ void load(const EpilogueArgs& e, const EpilogueSource& from, int64_t row, int64_t col, int left)
     {
         if constexpr (SUMS) x.template load<ENDS>(from.sums, row * e.cols + col, left);
         else x.template load<ENDS>(from.x, row * from.ld + col, left);
         if (e.residual) residual.template load<ENDS>(e.residual, row * e.residual_ld + col, left);
     }
-    // y of `valid` columns (zeros behind them); z goes out on the way.
+    // y, zeros behind the row's end; z goes out on the way.
     __device__ __forceinline__ void finish(const EpilogueArgs& e, const EpilogueSource& from, const Dropout& drop, const float (&bias)[8], int64_t row, int64_t col, int left,
                                            float (&y)[8])
     {
@@ -42,14 +50,16 @@ struct EpilogueOctet {
                 for (int j = 0; j < 8; ++j) y[j] += more.get(j);
             }
         }
+        if (e.bias) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] += bias[j];
-        if (e.z && left > 0) {
+            for (int j = 0; j < 8; ++j) y[j] += bias[j];
+        }
+        if (e.z) {
             Octet<DT> w;
             w.set(y);
-            w.store(e.z, row * e.z_ld + col, left);
+            put_octet<ENDS>(w, e.z, row * e.z_ld + col, left, e.large);
         }
-        activate(y, e.activation);
+        activate<ACT>(y, e.activation);
         drop.apply(y, (uint32_t)(col >> 3), (uint32_t)row);
         if (e.residual) {
             residual.template settle<ENDS>(left);
@@ -71,45 +81,39 @@ __device__ __forceinline__ void load_bias(const void* bias, int64_t col, int lef
     for (int j = 0; j < 8; ++j) x[j] = b.get(j);
 }
 
-// Rows as they are.  L lanes have a strip of 8 L columns, whose bias stays in registers, and kRows rows each at a time, whose loads go out together.
-template <int DT, bool SUMS, int L, Ends ENDS>
+// ---- forward --------------------------------------------------------------------------------------------------
+
+// Rows as they are.  L lanes have a strip of 8 L columns, whose bias stays in registers, and R rows each at a time, whose loads go out together.
+template <int DT, int ACT, bool SUMS, int L, int R, Ends ENDS>
 __global__ __launch_bounds__(256) void epilogue_rows_kernel(const EpilogueArgs e, const EpilogueSource from, uint32_t strips)
 {
-    constexpr int kRows = 4, kApartBy = 64 / L, kGroup = 4 * kRows * kApartBy;
-    const Dropout drop(e.drop);
+    constexpr int kApartBy = 64 / L, kGroup = 4 * R * kApartBy;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t col = ((int64_t)(blockIdx.x % strips) * L + lane % L) * 8;
     const int64_t behind = e.cols - col;
     const int left = behind < 8 ? (int)behind : 8;
-    float bias[8];
-    load_bias<DT, ENDS>(e.bias, col, left, bias);
     for (int64_t first = (int64_t)(blockIdx.x / strips) * kGroup; first < e.rows; first += (int64_t)(gridDim.x / strips) * kGroup) {
-        const int64_t row0 = first + wave * (kRows * kApartBy) + lane / L;
-        EpilogueOctet<DT, SUMS, ENDS> x[kRows];
+        const int64_t row0 = first + wave * (R * kApartBy) + lane / L;
+        EpilogueOctet<DT, ACT, SUMS, ENDS> x[R];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i)
+        for (int i = 0; i < R; ++i)
             if (row0 + i * kApartBy < e.rows) x[i].load(e, from, row0 + i * kApartBy, col, left);
+        float bias[8];
+        load_bias<DT, ENDS>(e.bias, col, left, bias);
+        const Dropout drop(e.drop);
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
+        for (int i = 0; i < R; ++i) {
             const int64_t row = row0 + i * kApartBy;
             if (row >= e.rows) continue;                  // (all 16 lanes of a block)
             float y[8];
             x[i].finish(e, from, drop, bias, row, col, left, y);
-            if (e.y && left > 0) {
+            if (e.y) {
                 Octet<DT> w;
                 w.set(y);
-                w.store(e.y, row * e.y_ld + col, left);
+                put_octet<ENDS>(w, e.y, row * e.y_ld + col, left, e.large);
             }
             if (e.y8.out) {
-                uint32_t most = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) most = max_of(most, magnitudes<ZI_FP32, false>(__float_as_uint(y[j])));
-                if (most >= kInfinity<ZI_FP32>) {
-                    most = 0;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) most = max_of(most, magnitudes<ZI_FP32, true>(__float_as_uint(y[j])));
-                }
-                const uint32_t byte = scale_byte(max_16(most));
+                const uint32_t byte = scale_byte(max_16(most_of(y)));
                 if (left > 0) {
                     const float scale = scale_of(byte);
                     *reinterpret_cast<u32x2*>(e.y8.out + row * e.y8.out_ld + col) =
@@ -135,82 +139,94 @@ struct TileThread {
 };
 
 // Tiles, whose transposed numbers are wanted.
-template <int DT, bool SUMS, Ends ENDS>
+template <int DT, int ACT, bool SUMS, Ends ENDS>
 __global__ __launch_bounds__(256) void epilogue_tiles_kernel(const EpilogueArgs e, const EpilogueSource from)
 {
-    __shared__ TileSpace<ZI_FP32> s_space;
-    const Dropout drop(e.drop);
+    __shared__ ResultSpace s_space;
     const TileThread at(e.cols, e.y8.tiles_across);
-    float bias[8];
-    load_bias<DT, ENDS>(e.bias, at.col, at.left, bias);
-    EpilogueOctet<DT, SUMS, ENDS> x[8];
+    float y[8][8];
+    const auto make = [&](auto whole) {               // (a tile with all its rows needs no look at them)
+        EpilogueOctet<DT, ACT, SUMS, ENDS> x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (at.row0 + i < e.rows) x[i].load(e, from, at.row0 + i, at.col, at.left);
-    Octet<ZI_FP32> y[8];
+        for (int i = 0; i < 8; ++i)
+            if (decltype(whole)::value || at.row0 + i < e.rows) x[i].load(e, from, at.row0 + i, at.col, at.left);
+        float bias[8];
+        load_bias<DT, ENDS>(e.bias, at.col, at.left, bias);
+        const Dropout drop(e.drop);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        y[i].clear();
-        if (at.row0 + i >= e.rows) continue;
-        float f[8];
-        x[i].finish(e, from, drop, bias, at.row0 + i, at.col, at.left, f);
-        y[i].set(f);
-        if (e.y && at.left > 0) {
-            Octet<DT> w;
-            w.set(f);
-            w.store(e.y, (at.row0 + i) * e.y_ld + at.col, at.left);
+        for (int i = 0; i < 8; ++i) {
+            if (!decltype(whole)::value && at.row0 + i >= e.rows) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[i][j] = 0.0f;
+                continue;
+            }
+            x[i].finish(e, from, drop, bias, at.row0 + i, at.col, at.left, y[i]);
+            if (e.y) {
+                Octet<DT> w;
+                w.set(y[i]);
+                put_octet<ENDS>(w, e.y, (at.row0 + i) * e.y_ld + at.col, at.left, e.large);
+            }
         }
-    }
-    quantize_tile<ZI_FP32, false>(e.y8, y, at.tile_row, at.tile_col, s_space);
+    };
+    if ((at.tile_row + 1) * kTile <= e.rows) make(std::true_type());
+    else make(std::false_type());
+    if (e.large) quantize_results<true>(e.y8, y, at.tile_row, at.tile_col, s_space);
+    else quantize_results<false>(e.y8, y, at.tile_row, at.tile_col, s_space);
 }
 
 // ---- backward -------------------------------------------------------------------------------------------------
 
 // dz of a tile, in all its forms, and the sums over the tile's rows, which a second kernel adds in their order.
-template <int DT, Ends ENDS>
+template <int DT, int ACT, Ends ENDS>
 __global__ __launch_bounds__(256) void epilogue_backward_kernel(const EpilogueBackwardArgs a, float* partials)
 {
-    __shared__ TileSpace<ZI_FP32> s_space;
+    __shared__ ResultSpace s_space;
     __shared__ float s_sum[4][kTile];
-    const Dropout drop(a.drop);
     const TileThread at(a.cols, a.dz8.tiles_across);
     const int t = threadIdx.x;
-    const bool with_z = a.activation != ZI_ACT_NONE;
-    Octet<DT> dy[8], z[8];
+    float dz[8][8], sum[8] = {};
+    const auto make = [&](auto whole) {
+        Octet<DT> dy[8], z[ACT == ZI_ACT_NONE ? 1 : 8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (at.row0 + i >= a.rows) continue;
-        dy[i].template load<ENDS>(a.dy, (at.row0 + i) * a.dy_ld + at.col, at.left);
-        if (with_z) z[i].template load<ENDS>(a.z, (at.row0 + i) * a.z_ld + at.col, at.left);
-    }
-    Octet<ZI_FP32> dz[8];
-    float sum[8] = {};
+        for (int i = 0; i < 8; ++i)
+            if (decltype(whole)::value || at.row0 + i < a.rows) {
+                dy[i].template load<ENDS>(a.dy, (at.row0 + i) * a.dy_ld + at.col, at.left);
+                if constexpr (ACT != ZI_ACT_NONE)
+                    if (ACT != kAnyActivation || a.z) z[i].template load<ENDS>(a.z, (at.row0 + i) * a.z_ld + at.col, at.left);
+            }
+        const Dropout drop(a.drop);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        dz[i].clear();
-        const int64_t row = at.row0 + i;
-        if (row >= a.rows) continue;
-        dy[i].template settle<ENDS>(at.left);
-        float f[8];
+        for (int i = 0; i < 8; ++i) {
+            const int64_t row = at.row0 + i;
+            if (!decltype(whole)::value && row >= a.rows) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = dy[i].get(j);
-        drop.apply(f, (uint32_t)(at.col >> 3), (uint32_t)row);
-        if (with_z) {
-            z[i].template settle<ENDS>(at.left);
-            with_activation(a.activation, [&](auto act) {
+                for (int j = 0; j < 8; ++j) dz[i][j] = 0.0f;
+                continue;
+            }
+            dy[i].template settle<ENDS>(at.left);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = with_derivative<decltype(act)::value>(f[j], z[i].get(j));
-            });
+            for (int j = 0; j < 8; ++j) dz[i][j] = dy[i].get(j);
+            drop.apply(dz[i], (uint32_t)(at.col >> 3), (uint32_t)row);
+            if constexpr (ACT != ZI_ACT_NONE) {
+                if (ACT != kAnyActivation || a.z) {
+                    float f[8];
+                    z[i].template settle<ENDS>(at.left);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] = z[i].get(j);
+                    derive<ACT>(dz[i], f, a.activation);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += dz[i][j];
+            if (a.dz) {
+                Octet<DT> w;
+                w.set(dz[i]);
+                put_octet<ENDS>(w, a.dz, row * a.dz_ld + at.col, at.left, a.large);
+            }
         }
-        dz[i].set(f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] += f[j];
-        if (a.dz && at.left > 0) {
-            Octet<DT> w;
-            w.set(f);
-            w.store(a.dz, row * a.dz_ld + at.col, at.left);
-        }
-    }
+    };
+    if ((at.tile_row + 1) * kTile <= a.rows) make(std::true_type());
+    else make(std::false_type());
     if (a.dbias) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -222,7 +238,10 @@ __global__ __launch_bounds__(256) void epilogue_backward_kernel(const EpilogueBa
         const int64_t col = at.tile_col * kTile + t;
         if (t < kTile && col < a.cols) partials[at.tile_row * a.cols + col] = s_sum[0][t] + s_sum[1][t] + s_sum[2][t] + s_sum[3][t];
     }
-    if (a.dz8.out || a.dz8.turned) quantize_tile<ZI_FP32, false>(a.dz8, dz, at.tile_row, at.tile_col, s_space);
+    if (a.dz8.out || a.dz8.turned) {
+        if (a.large) quantize_results<true>(a.dz8, dz, at.tile_row, at.tile_col, s_space);
+        else quantize_results<false>(a.dz8, dz, at.tile_row, at.tile_col, s_space);
+    }
 }
 
 // ---- which kernel ---------------------------------------------------------------------------------------------
@@ -230,51 +249,86 @@ __global__ __launch_bounds__(256) void epilogue_backward_kernel(const EpilogueBa
 namespace {
 
 constexpr int64_t kMostGroups = (int64_t)1 << 20;     // workgroups over rows
+#ifndef ZI_R
+#define ZI_R 4
+#endif
+constexpr int kRowsAtATime = ZI_R;
+// Outputs of more do not stay in the memory-side cache for whoever reads them next, and pass it by.
+constexpr int64_t kLargeBytes = (int64_t)96 << 20;
 
-template <int DT, bool SUMS, Ends ENDS>
+template <int N>
+using int_type = std::integral_constant<int, N>;
+
+// f with what kernels of 16-bit matrices are made for: the activation and how rows end.
+template <typename F>
+void with_kind(int activation, int64_t cols, const F& f)
+{
+    const auto of = [&](auto act) {
+        if (cols % 8 == 0) f(act, std::integral_constant<Ends, Ends::kWhole>());
+        else f(act, std::integral_constant<Ends, Ends::kMoved>());
+    };
+    if (cols < 8) return f(int_type<kAnyActivation>(), std::integral_constant<Ends, Ends::kApart>());
+    switch (activation) {
+    case ZI_ACT_NONE: return of(int_type<ZI_ACT_NONE>());
+    case ZI_ACT_RELU: return of(int_type<ZI_ACT_RELU>());
+    case ZI_ACT_GELU: return of(int_type<ZI_ACT_GELU>());
+    case ZI_ACT_GELU_TANH: return of(int_type<ZI_ACT_GELU_TANH>());
+    case ZI_ACT_SILU: return of(int_type<ZI_ACT_SILU>());
+    }
+}
+
+template <int DT, int ACT, bool SUMS, Ends ENDS>
 void launch_forward(const EpilogueArgs& e, const EpilogueSource& from, hipStream_t s)
 {
     const int64_t down = (e.rows + kTile - 1) / kTile;
     if (e.y8.turned) {
-        hipLaunchKernelGGL((epilogue_tiles_kernel<DT, SUMS, ENDS>), dim3((unsigned)(e.y8.tiles_across * down)), dim3(256), 0, s, e, from);
+        hipLaunchKernelGGL((epilogue_tiles_kernel<DT, ACT, SUMS, ENDS>), dim3((unsigned)(e.y8.tiles_across * down)), dim3(256), 0, s, e, from);
         return;
     }
-    const auto rows = [&](auto lanes, auto kernel) {
-        constexpr int kLanes = decltype(lanes)::value;
-        const int64_t strips = (e.cols + 8 * kLanes - 1) / (8 * kLanes), groups = (e.rows + 1024 / kLanes - 1) / (1024 / kLanes);
+    const auto rows = [&](int lanes, int at_a_time, auto kernel) {
+        const int64_t strips = (e.cols + 8 * lanes - 1) / (8 * lanes), each = 4 * (64 / lanes) * at_a_time, groups = (e.rows + each - 1) / each;
         const int64_t most = strips < kMostGroups ? kMostGroups / strips : 1;
         hipLaunchKernelGGL(kernel, dim3((unsigned)(strips * (groups < most ? groups : most))), dim3(256), 0, s, e, from, (uint32_t)strips);
     };
-    if (e.cols <= 128) rows(std::integral_constant<int, 16>(), epilogue_rows_kernel<DT, SUMS, 16, ENDS>);
-    else rows(std::integral_constant<int, 64>(), epilogue_rows_kernel<DT, SUMS, 64, ENDS>);
+    if (ENDS == Ends::kApart || e.cols <= 128) rows(16, 2, epilogue_rows_kernel<DT, ACT, SUMS, 16, 2, ENDS>);
+    else if constexpr (ENDS != Ends::kApart) rows(64, kRowsAtATime, epilogue_rows_kernel<DT, ACT, SUMS, 64, kRowsAtATime, ENDS>);
 }
-template <int DT, bool SUMS>
+
+template <int DT>
 void launch_forward_of(const EpilogueArgs& e, const EpilogueSource& from, hipStream_t s)
 {
-    if (e.cols % 8 == 0) launch_forward<DT, SUMS, Ends::kWhole>(e, from, s);
-    else if (e.cols > 8) launch_forward<DT, SUMS, Ends::kMoved>(e, from, s);
-    else launch_forward<DT, SUMS, Ends::kApart>(e, from, s);
+    if (!from.x) {
+        if (e.cols % 8 == 0) launch_forward<DT, kAnyActivation, true, Ends::kWhole>(e, from, s);
+        else if (e.cols > 8) launch_forward<DT, kAnyActivation, true, Ends::kMoved>(e, from, s);
+        else launch_forward<DT, kAnyActivation, true, Ends::kApart>(e, from, s);
+        return;
+    }
+    with_kind(e.activation, e.cols, [&](auto act, auto ends) { launch_forward<DT, decltype(act)::value, false, decltype(ends)::value>(e, from, s); });
 }
 template <int DT>
 void launch_backward_of(const EpilogueBackwardArgs& a, float* partials, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.dz8.tiles_across * ((a.rows + kTile - 1) / kTile))), block(256);
-    if (a.cols % 8 == 0) hipLaunchKernelGGL((epilogue_backward_kernel<DT, Ends::kWhole>), grid, block, 0, s, a, partials);
-    else if (a.cols > 8) hipLaunchKernelGGL((epilogue_backward_kernel<DT, Ends::kMoved>), grid, block, 0, s, a, partials);
-    else hipLaunchKernelGGL((epilogue_backward_kernel<DT, Ends::kApart>), grid, block, 0, s, a, partials);
+    with_kind(a.activation, a.cols, [&](auto act, auto ends) {
+        hipLaunchKernelGGL((epilogue_backward_kernel<DT, decltype(act)::value, decltype(ends)::value>), grid, block, 0, s, a, partials);
+    });
 }
 
 }  // namespace
 
-hipError_t launch_epilogue(const EpilogueArgs& e, const EpilogueSource& from, int dtype, hipStream_t s)
+hipError_t launch_epilogue(const EpilogueArgs& given, const EpilogueSource& from, int dtype, hipStream_t s)
 {
-    if (dtype == ZI_BF16) from.x ? launch_forward_of<ZI_BF16, false>(e, from, s) : launch_forward_of<ZI_BF16, true>(e, from, s);
-    else from.x ? launch_forward_of<ZI_FP16, false>(e, from, s) : launch_forward_of<ZI_FP16, true>(e, from, s);
+    EpilogueArgs e = given;
+    e.large = e.rows * e.cols * ((e.z ? 2 : 0) + (e.y ? 2 : 0) + (e.y8.out ? 1 : 0) + (e.y8.turned ? 1 : 0)) >= kLargeBytes;
+    if (dtype == ZI_BF16) launch_forward_of<ZI_BF16>(e, from, s);
+    else launch_forward_of<ZI_FP16>(e, from, s);
     return hipGetLastError();
 }
 
-hipError_t launch_epilogue_backward(const EpilogueBackwardArgs& a, int dtype, float* partials, hipStream_t s)
+hipError_t launch_epilogue_backward(const EpilogueBackwardArgs& given, int dtype, float* partials, hipStream_t s)
 {
+    EpilogueBackwardArgs a = given;
+    a.large = a.rows * a.cols * ((a.dz ? 2 : 0) + (a.dz8.out ? 1 : 0) + (a.dz8.turned ? 1 : 0)) >= kLargeBytes;
     const int64_t down = (a.rows + kTile - 1) / kTile;
     if (a.rows > 0) {
         if (dtype == ZI_BF16) launch_backward_of<ZI_BF16>(a, partials, s);

@@ -49,7 +49,7 @@ __device__ __forceinline__ float activated(float z)
     } else if constexpr (ACT == ZI_ACT_SILU) return z * sigmoid_of_exponent(-kLog2E * z);
     else return z;
 }
-// dy times the derivative.  (Where a sigmoid s is 0 or 1, s - s^2 is 0, which its large factors are multiplied to one after the other.)
+// dy times the derivative.  (Where a sigmoid s is 0 or 1, s (1 - s) is 0, which its large factors are multiplied to one after the other.)
 template <int ACT>
 __device__ __forceinline__ float with_derivative(float dy, float z)
 {
@@ -59,9 +59,10 @@ __device__ __forceinline__ float with_derivative(float dy, float z)
         const float phi = normal_cdf(z, e);
         return dy * __builtin_fmaf(z * e, 0.398942280f, phi);
     } else if constexpr (ACT == ZI_ACT_GELU_TANH) {
-        const float z2 = __builtin_fminf(z * z, 256.0f);                    // (beyond 16, s - s^2 is 0)
-        const float s = sigmoid_of_exponent(z * __builtin_fmaf(z * z, -kLog2E * kTanhCube, -kLog2E * kTanh));
-        return dy * __builtin_fmaf(__builtin_fmaf(-s, s, s) * z, __builtin_fmaf(z2, 3.0f * kTanhCube, kTanh), s);
+        // 1 - s is exp(..) s, without the rounding of s near 1, which the slope of the cube (up to 50) would make much of; 1 where exp is infinite.
+        const float z2 = z * z, e = exp2_of(z * __builtin_fmaf(z2, -kLog2E * kTanhCube, -kLog2E * kTanh)), s = inverse(1.0f + e), rest = __builtin_fminf(e * s, 1.0f);
+        const float slope = __builtin_fmaf(__builtin_fminf(z2, 256.0f), 3.0f * kTanhCube, kTanh);                // (beyond 16, s (1 - s) is 0)
+        return dy * __builtin_fmaf(s * rest * z, slope, s);
     } else if constexpr (ACT == ZI_ACT_SILU) {
         const float s = sigmoid_of_exponent(-kLog2E * z);
         return dy * __builtin_fmaf(__builtin_fmaf(-s, s, s), z, s);
@@ -78,15 +79,47 @@ __device__ __forceinline__ void with_activation(int activation, const F& f)
     case ZI_ACT_SILU: return f(std::integral_constant<int, ZI_ACT_SILU>());
     }
 }
+// Eight elements, of an activation that is known or (ACT kAnyActivation) is not.
+constexpr int kAnyActivation = -1;
+template <int ACT>
 __device__ __forceinline__ void activate(float (&x)[8], int activation)
 {
-    with_activation(activation, [&](auto act) {
+    if constexpr (ACT != kAnyActivation) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = activated<decltype(act)::value>(x[j]);
-    });
+        for (int j = 0; j < 8; ++j) x[j] = activated<ACT>(x[j]);
+    } else {
+        with_activation(activation, [&](auto act) { activate<decltype(act)::value>(x, activation); });
+    }
+}
+template <int ACT>
+__device__ __forceinline__ void derive(float (&dy)[8], const float (&z)[8], int activation)
+{
+    if constexpr (ACT != kAnyActivation) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dy[j] = with_derivative<ACT>(dy[j], z[j]);
+    } else {
+        with_activation(activation, [&](auto act) { derive<decltype(act)::value>(dy, z, activation); });
+    }
+}
+
+// Largest finite magnitude of N numbers, its fp32 bits.  (A NaN has no part in a maximum; only where an infinity is found they are looked through again.)
+template <int N>
+__device__ __forceinline__ uint32_t most_of(const float (&x)[N])
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < N; j += 2) most = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(x[j]), __builtin_fabsf(x[j + 1])), most);
+    if (most == __builtin_inff()) {
+        most = 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) most = __builtin_fabsf(x[j]) < __builtin_inff() ? __builtin_fmaxf(most, __builtin_fabsf(x[j])) : most;
+    }
+    return __float_as_uint(most);
 }
 
 // ---- dropout --------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t xor_of(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
 
 // Philox4x32-10: ten rounds, of two 32 x 32 -> 64 multiplications each, on a counter of four words.  One call is eight columns' numbers.
 struct Dropout {
@@ -105,9 +138,9 @@ struct Dropout {
 #pragma unroll
         for (int i = 0; i < 10; ++i) {
             const uint64_t a = (uint64_t)x0 * 0xD2511F53u, b = (uint64_t)x2 * 0xCD9E8D57u;
-            x0 = (uint32_t)(b >> 32) ^ x1 ^ k0;
+            x0 = xor_of((uint32_t)(b >> 32), x1, k0);
             x1 = (uint32_t)b;
-            x2 = (uint32_t)(a >> 32) ^ x3 ^ k1;
+            x2 = xor_of((uint32_t)(a >> 32), x3, k1);
             x3 = (uint32_t)a;
             k0 += 0x9E3779B9u;
             k1 += 0xBB67AE85u;

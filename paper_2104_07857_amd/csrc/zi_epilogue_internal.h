@@ -24,6 +24,7 @@ struct EpilogueArgs {
     DropoutArgs drop;
     int32_t activation;
     QuantizeArgs y8;              // its out and turned; x and ld are not used
+    bool large;                   // outputs are streamed past the caches
 };
 // Where x comes from: 16 bits, or the sums that a product left in parts of rows x cols.
 struct EpilogueSource {
@@ -48,6 +49,7 @@ struct EpilogueBackwardArgs {
     DropoutArgs drop;
     int32_t activation;
     QuantizeArgs dz8;
+    bool large;
 };
 hipError_t launch_epilogue_backward(const EpilogueBackwardArgs& a, int dtype, float* workspace, hipStream_t s);
 
