@@ -102,6 +102,29 @@ __device__ __forceinline__ void derive(float (&dy)[8], const float (&z)[8], int 
     }
 }
 
+// The product's kernels know less of the activation, as each is made for several sizes of tile too (and a branch among all of them, with a tile's sums in registers, costs registers that
+// there are not): its kind, with numbers that are the same in all lanes.
+enum class ActivationKind { kFloor, kSigmoid, kNormal };       // none and relu; gelu_tanh and silu; gelu
+struct ActivationForm {
+    float a, b;
+    __device__ __forceinline__ explicit ActivationForm(int activation)
+        : a(activation == ZI_ACT_GELU_TANH ? -kLog2E * kTanh : activation == ZI_ACT_SILU ? -kLog2E : activation == ZI_ACT_RELU ? 0.0f : -__builtin_inff()),
+          b(activation == ZI_ACT_GELU_TANH ? -kLog2E * kTanhCube : 0.0f)
+    {
+    }
+};
+template <ActivationKind KIND>
+__device__ __forceinline__ float activated_as(const ActivationForm& f, float z)
+{
+    if constexpr (KIND == ActivationKind::kFloor) return z < f.a ? 0.0f : z;
+    else if constexpr (KIND == ActivationKind::kSigmoid) return z * sigmoid_of_exponent(z * __builtin_fmaf(__builtin_fminf(z * z, 0x1p100f), f.b, f.a));      // (0 times infinity would be NaN)
+    else return activated<ZI_ACT_GELU>(z);
+}
+inline ActivationKind kind_of(int activation)
+{
+    return activation == ZI_ACT_GELU ? ActivationKind::kNormal : activation == ZI_ACT_GELU_TANH || activation == ZI_ACT_SILU ? ActivationKind::kSigmoid : ActivationKind::kFloor;
+}
+
 // Largest finite magnitude of N numbers, its fp32 bits.  (A NaN has no part in a maximum; only where an infinity is found they are looked through again.)
 template <int N>
 __device__ __forceinline__ uint32_t most_of(const float (&x)[N])
