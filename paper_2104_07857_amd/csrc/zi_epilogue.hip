@@ -38,18 +38,9 @@ struct EpilogueOctet {
     __device__ __forceinline__ void finish(const EpilogueArgs& e, const EpilogueSource& from, const Dropout& drop, const float (&bias)[8], int64_t row, int64_t col, int left,
                                            float (&y)[8])
     {
-        x.template settle<ENDS>(left);
+        if constexpr (!SUMS) x.template settle<ENDS>(left);
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = x.get(j);
-        if constexpr (SUMS) {
-            for (uint32_t i = 1; i < from.parts; ++i) {
-                Octet<ZI_FP32> more;
-                more.template load<ENDS>(from.sums, ((int64_t)i * e.rows + row) * e.cols + col, left);
-                more.template settle<ENDS>(left);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] += more.get(j);
-            }
-        }
         if (e.bias) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += bias[j];
@@ -68,6 +59,33 @@ struct EpilogueOctet {
         }
     }
 };
+// The other parts' sums, in their order, for octets of R rows: with few rows three parts at a time are under way (there are 2, 4, 8 or 16), with more two.
+template <int R, int APART, int DT, int ACT, Ends ENDS>
+__device__ __forceinline__ void add_parts(EpilogueOctet<DT, ACT, true, ENDS> (&x)[R], const EpilogueArgs& e, const EpilogueSource& from, int64_t row0, int64_t col, int left)
+{
+    constexpr int kParts = R <= 2 ? 3 : 2;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (row0 + r * APART < e.rows) x[r].x.template settle<ENDS>(left);
+    for (uint32_t first = 1; first < from.parts; first += kParts) {
+        Octet<ZI_FP32> more[kParts][R];
+#pragma unroll
+        for (int i = 0; i < kParts; ++i)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (first + i < from.parts && row0 + r * APART < e.rows)
+                    more[i][r].template load<ENDS>(from.sums, ((int64_t)(first + i) * e.rows + row0 + r * APART) * e.cols + col, left);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (first + i >= from.parts || row0 + r * APART >= e.rows) continue;
+                more[i][r].template settle<ENDS>(left);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[r].x.w[j] = __float_as_uint(x[r].x.get(j) + more[i][r].get(j));
+            }
+    }
+}
 template <int DT, Ends ENDS>
 __device__ __forceinline__ void load_bias(const void* bias, int64_t col, int left, float (&x)[8])
 {
@@ -101,6 +119,7 @@ __global__ __launch_bounds__(256) void epilogue_rows_kernel(const EpilogueArgs e
         float bias[8];
         load_bias<DT, ENDS>(e.bias, col, left, bias);
         const Dropout drop(e.drop);
+        if constexpr (SUMS) add_parts<R, kApartBy>(x, e, from, row0, col, left);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int64_t row = row0 + i * kApartBy;
@@ -153,6 +172,7 @@ __global__ __launch_bounds__(256) void epilogue_tiles_kernel(const EpilogueArgs 
         float bias[8];
         load_bias<DT, ENDS>(e.bias, at.col, at.left, bias);
         const Dropout drop(e.drop);
+        if constexpr (SUMS) add_parts<8, 1>(x, e, from, at.row0, at.col, at.left);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (!decltype(whole)::value && at.row0 + i >= e.rows) {
@@ -176,7 +196,8 @@ __global__ __launch_bounds__(256) void epilogue_tiles_kernel(const EpilogueArgs 
 
 // ---- backward -------------------------------------------------------------------------------------------------
 
-// dz of a tile, in all its forms, and the sums over the tile's rows, which a second kernel adds in their order.
+// dz of a tile, in all its forms, and the sums over the tile's rows, which a second kernel adds in their order.  Where there is but one row of tiles they are dbias: 100 x 4096 in one
+// kernel 5.1 us, in two 6.9; with two rows of tiles one after the other in a workgroup it is 6.8 against 6.7 (and, with 8-bit outputs, 12.2 against 9.8).
 template <int DT, int ACT, Ends ENDS>
 __global__ __launch_bounds__(256) void epilogue_backward_kernel(const EpilogueBackwardArgs a, float* partials)
 {
@@ -236,7 +257,20 @@ __global__ __launch_bounds__(256) void epilogue_backward_kernel(const EpilogueBa
         }
         __syncthreads();
         const int64_t col = at.tile_col * kTile + t;
-        if (t < kTile && col < a.cols) partials[at.tile_row * a.cols + col] = s_sum[0][t] + s_sum[1][t] + s_sum[2][t] + s_sum[3][t];
+        if (t < kTile && col < a.cols) {
+            const float x = s_sum[0][t] + s_sum[1][t] + s_sum[2][t] + s_sum[3][t];
+            if (a.rows > kTile) {
+                partials[at.tile_row * a.cols + col] = x;
+            } else if (a.dbias_dtype == ZI_FP32) {
+                float* to = static_cast<float*>(a.dbias) + col;
+                *to = a.accumulate ? *to + x : x;
+            } else {
+                uint16_t* to = static_cast<uint16_t*>(a.dbias) + col;
+                Octet<DT> old;
+                old.w[0] = *to;
+                *to = (uint16_t)Octet<DT>::pair(a.accumulate ? old.get(0) + x : x, 0.0f);
+            }
+        }
     }
     if (a.dz8.out || a.dz8.turned) {
         if (a.large) quantize_results<true>(a.dz8, dz, at.tile_row, at.tile_col, s_space);
@@ -249,10 +283,7 @@ __global__ __launch_bounds__(256) void epilogue_backward_kernel(const EpilogueBa
 namespace {
 
 constexpr int64_t kMostGroups = (int64_t)1 << 20;     // workgroups over rows
-#ifndef ZI_R
-#define ZI_R 4
-#endif
-constexpr int kRowsAtATime = ZI_R;
+constexpr int kRowsAtATime = 4;
 // Outputs of more do not stay in the memory-side cache for whoever reads them next, and pass it by.
 constexpr int64_t kLargeBytes = (int64_t)96 << 20;
 
@@ -290,8 +321,9 @@ void launch_forward(const EpilogueArgs& e, const EpilogueSource& from, hipStream
         const int64_t most = strips < kMostGroups ? kMostGroups / strips : 1;
         hipLaunchKernelGGL(kernel, dim3((unsigned)(strips * (groups < most ? groups : most))), dim3(256), 0, s, e, from, (uint32_t)strips);
     };
+    constexpr int kEach = SUMS ? 1 : kRowsAtATime;
     if (ENDS == Ends::kApart || e.cols <= 128) rows(16, 2, epilogue_rows_kernel<DT, ACT, SUMS, 16, 2, ENDS>);
-    else if constexpr (ENDS != Ends::kApart) rows(64, kRowsAtATime, epilogue_rows_kernel<DT, ACT, SUMS, 64, kRowsAtATime, ENDS>);
+    else if constexpr (ENDS != Ends::kApart) rows(64, kEach, epilogue_rows_kernel<DT, ACT, SUMS, 64, kEach, ENDS>);
 }
 
 template <int DT>
@@ -334,7 +366,7 @@ hipError_t launch_epilogue_backward(const EpilogueBackwardArgs& given, int dtype
         if (dtype == ZI_BF16) launch_backward_of<ZI_BF16>(a, partials, s);
         else launch_backward_of<ZI_FP16>(a, partials, s);
         const hipError_t err = hipGetLastError();
-        if (err != hipSuccess) return err;
+        if (err != hipSuccess || down == 1) return err;
     }
     return a.dbias ? launch_column_sums(partials, (int)down, a.cols, a.dbias, a.dbias_dtype, a.accumulate, s) : hipSuccess;
 }

@@ -51,10 +51,13 @@ struct MatmulArgs {
     int32_t a_shift, b_shift;     // row >> shift is its row of scales: 0 or 7
 };
 struct MatmulPlan {
-    int shape;               // of the tiles, or -1: the kernel for few rows
+    int shape;               // of the tiles, or kFewRows: the kernel for few rows
     uint32_t parts, part_steps;      // workgroups that share out k, and their steps of 128
 };
+constexpr int kFewRows = -1;
 MatmulPlan plan_fp8_matmul(int64_t m, int64_t n, int64_t k);
+// The same among shapes from `first` on, of which more than the smallest come in one part; and the time that it is expected to take, in us.
+MatmulPlan plan_fp8_matmul_from(int64_t m, int64_t n, int64_t k, int first, float& estimate);
 hipError_t launch_fp8_matmul(const MatmulArgs& a, int dtype, float* partials, hipStream_t s);
 
 }  // namespace zi

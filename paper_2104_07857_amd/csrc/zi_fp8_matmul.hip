@@ -94,12 +94,17 @@ static float few_rows_estimate(int64_t m, int64_t n, int64_t k)
 // these same products it is 0.4 % slower than that on the average; on others it was not measured.
 MatmulPlan plan_fp8_matmul(int64_t m, int64_t n, int64_t k)
 {
+    float estimate;
+    return plan_fp8_matmul_from(m, n, k, kFewRows, estimate);
+}
+MatmulPlan plan_fp8_matmul_from(int64_t m, int64_t n, int64_t k, int first, float& least)
+{
     const int64_t steps = (k + kStep - 1) / kStep;
     const float stream = ((float)m + (float)n) * (float)k + kOutput * (float)m * (float)n;
-    MatmulPlan best{-1, 1, (uint32_t)((steps + 3) / 4 * 4)};
-    float least = INFINITY;
-    if (m <= 32) least = few_rows_estimate(m, n, k);
-    for (int i = 0; i < kShapes; ++i) {
+    MatmulPlan best{kFewRows, 1, (uint32_t)((steps + 3) / 4 * 4)};
+    least = INFINITY;
+    if (m <= 32 && first == kFewRows) least = few_rows_estimate(m, n, k);
+    for (int i = first > 0 ? first : 0; i < kShapes; ++i) {
         const TileShape& t = kShape[i];
         const int64_t tiles = ((m + t.rows - 1) / t.rows) * ((n + t.cols - 1) / t.cols);
         for (int64_t parts = 1; parts <= (i == 0 ? 16 : 1); parts *= 2) {

@@ -14,11 +14,84 @@ hipError_t launch_fp8_matmul_epilogue_tiles<ActivationKind::kNormal>(const Matmu
 
 namespace {
 
-// What the tiles of a plan can put out themselves: blocks of 128 rows or columns have to be a workgroup's own.
-bool makes_all(const MatmulPlan& plan, int outputs8)
+// Few rows, whose sums become 16-bit outputs here, element by element.  (Of eight numbers that dropout's generator makes at a time one is used; blocks of 128 columns are eight
+// workgroups', so that outputs in 8 bits are left to a second kernel.)
+template <int DT, int FA, int W>
+__global__ __launch_bounds__(64 * W) void fp8_matmul_few_epilogue_kernel(const MatmulArgs p, const EpilogueArgs e)
 {
-    if (plan.shape < 0 || plan.parts > 1) return false;
-    return !(outputs8 & ZI_EPILOGUE_TURNED ? plan.shape < 2 : outputs8 & ZI_EPILOGUE_Y8 ? plan.shape < 1 : false);
+    __shared__ float s_sum[W][FA][16][17];
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const auto of = [](const void* base, int64_t at) {
+        Octet<DT> x;
+        x.w[0] = static_cast<const uint16_t*>(base)[at];
+        return x.get(0);
+    };
+    const auto put = [](void* base, int64_t at, float x) { static_cast<uint16_t*>(base)[at] = (uint16_t)Octet<DT>::pair(x, 0.0f); };
+    const Dropout drop(e.drop);
+    constexpr int kEach = FA * 256 > 64 * W ? FA * 256 / (64 * W) : 1;
+    float bias[kEach], residual[kEach];                 // (under way while the product is made)
+    const auto place = [&](int i, int& f, int& m, int& n) {
+        const int t = threadIdx.x + i * 64 * W;
+        f = t >> 8;
+        m = (t >> 4) & 15;
+        n = t & 15;
+        return f < FA && 16 * f + m < p.m && n0 + n < p.n;
+    };
+    int f, m, n;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        bias[i] = residual[i] = 0.0f;
+        if (!place(i, f, m, n)) continue;
+        if (e.bias) bias[i] = of(e.bias, n0 + n);
+        if (e.residual) residual[i] = of(e.residual, (16 * f + m) * e.residual_ld + n0 + n);
+    }
+    multiply_few<FA, W>(p, n0, s_sum);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (!place(i, f, m, n)) continue;
+        const int64_t row = 16 * f + m, col = n0 + n;
+        float x = sum_of_few<FA, W>(s_sum, f, m, n);
+        if (e.bias) x += bias[i];
+        if (e.z) put(e.z, row * e.z_ld + col, x);
+        if (!e.y) continue;
+        with_activation(e.activation, [&](auto act) { x = activated<decltype(act)::value>(x); });
+        if (drop.active()) {
+            const u32x4 w = drop.numbers((uint32_t)(col >> 3), (uint32_t)row);
+            const int j = (int)(col & 7);
+            const uint32_t word = j < 4 ? (j < 2 ? w[0] : w[1]) : (j < 6 ? w[2] : w[3]);
+            x = (j & 1 ? word >> 16 : word & 0xFFFFu) >= drop.threshold ? x * drop.scale : 0.0f;
+        }
+        if (e.residual) x += residual[i];
+        put(e.y, row * e.y_ld + col, x);
+    }
+}
+template <int DT>
+hipError_t launch_few_epilogue(const MatmulArgs& a, const EpilogueArgs& e, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.n + 15) / 16)), block(512);
+    if (a.m <= 16) hipLaunchKernelGGL((fp8_matmul_few_epilogue_kernel<DT, 1, 8>), grid, block, 0, s, a, e);
+    else hipLaunchKernelGGL((fp8_matmul_few_epilogue_kernel<DT, 2, 8>), grid, block, 0, s, a, e);
+    return hipGetLastError();
+}
+
+// How a product is made, and whether all of its outputs come from there: tiles put out blocks of 128 rows or columns that are a workgroup's own.  Where the fastest way to the sums is none
+// to the outputs, a second kernel that reads the sums again stands against the fastest way that is.
+struct EpiloguePlan {
+    MatmulPlan plan;
+    bool whole;
+};
+constexpr float kSecond = 2.5f, kSecondStream = 4.5e6f, kWhole = 1.5f;      // us of the second kernel; bytes a us; us of blocks made in tiles
+EpiloguePlan plan_epilogue(int64_t m, int64_t n, int64_t k, int outputs8)
+{
+    const int first = outputs8 & ZI_EPILOGUE_TURNED ? 2 : outputs8 & ZI_EPILOGUE_Y8 ? 1 : kFewRows;
+    float any, whole;
+    const MatmulPlan plan = plan_fp8_matmul_from(m, n, k, kFewRows, any);
+    if (plan.parts == 1 && plan.shape >= first) return {plan, true};
+    const MatmulPlan other = plan_fp8_matmul_from(m, n, k, first > 0 ? first : 0, whole);
+    // (The estimate for parts has their sum in it already.)  1 x 16384 x 4096 to 8 bits: in two kernels 15.0 us, whole in tiles of 64 x 128 17.3; 2048 x 2048 x 2048 transposed 22 and 14.
+    const float second = plan.parts > 1 ? 0.0f : kSecond + 8.0f * (float)m * (float)n / kSecondStream;
+    if (other.parts == 1 && whole + kWhole <= any + second) return {other, true};
+    return {plan, false};
 }
 
 // Sums in a workspace, for a kernel over rows or tiles to go on with.
@@ -48,24 +121,25 @@ hipError_t launch_sums(const MatmulArgs& a, const MatmulPlan& plan, float* sums,
 
 size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int outputs8)
 {
-    const MatmulPlan plan = plan_fp8_matmul(m, n, k);
-    return makes_all(plan, outputs8) ? 0 : plan.parts * (size_t)m * (size_t)n;
+    const EpiloguePlan p = plan_epilogue(m, n, k, outputs8);
+    return p.whole ? 0 : p.plan.parts * (size_t)m * (size_t)n;
 }
 
 hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpilogueArgs& e, int dtype, float* workspace, hipStream_t s)
 {
-    const MatmulPlan plan = plan_fp8_matmul(a.m, a.n, a.k);
-    const int outputs8 = (e.y8.out ? ZI_EPILOGUE_Y8 : 0) | (e.y8.turned ? ZI_EPILOGUE_TURNED : 0);
-    if (makes_all(plan, outputs8)) {
-        switch (kind_of(e.activation)) {
-        case ActivationKind::kFloor: return launch_fp8_matmul_epilogue_tiles<ActivationKind::kFloor>(a, plan, e, dtype, s);
-        case ActivationKind::kSigmoid: return launch_fp8_matmul_epilogue_tiles<ActivationKind::kSigmoid>(a, plan, e, dtype, s);
-        case ActivationKind::kNormal: return launch_fp8_matmul_epilogue_tiles<ActivationKind::kNormal>(a, plan, e, dtype, s);
-        }
+    const EpiloguePlan p = plan_epilogue(a.m, a.n, a.k, (e.y8.out ? ZI_EPILOGUE_Y8 : 0) | (e.y8.turned ? ZI_EPILOGUE_TURNED : 0));
+    if (!p.whole) {
+        const hipError_t err = launch_sums(a, p.plan, workspace, s);
+        if (err != hipSuccess) return err;
+        return launch_epilogue(e, EpilogueSource{nullptr, 0, workspace, p.plan.parts}, dtype, s);
     }
-    const hipError_t err = launch_sums(a, plan, workspace, s);
-    if (err != hipSuccess) return err;
-    return launch_epilogue(e, EpilogueSource{nullptr, 0, workspace, plan.parts}, dtype, s);
+    if (p.plan.shape == kFewRows) return dtype == ZI_BF16 ? launch_few_epilogue<ZI_BF16>(a, e, s) : launch_few_epilogue<ZI_FP16>(a, e, s);
+    switch (kind_of(e.activation)) {
+    case ActivationKind::kFloor: return launch_fp8_matmul_epilogue_tiles<ActivationKind::kFloor>(a, p.plan, e, dtype, s);
+    case ActivationKind::kSigmoid: return launch_fp8_matmul_epilogue_tiles<ActivationKind::kSigmoid>(a, p.plan, e, dtype, s);
+    case ActivationKind::kNormal: break;
+    }
+    return launch_fp8_matmul_epilogue_tiles<ActivationKind::kNormal>(a, p.plan, e, dtype, s);
 }
 
 }  // namespace zi

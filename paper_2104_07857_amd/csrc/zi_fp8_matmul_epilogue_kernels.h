@@ -356,8 +356,7 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
             for (int s = 0; s < kEach; ++s) {
                 const uint32_t byte = scale_byte(most[s]);
                 const int c = column(in * kEach + s);
-                // 1 / scale: what rows of one column are multiplied by, whose neighbours have scales of their own
-                scales[c] = __uint_as_float(byte < 254 ? (254 - byte) << 23 : 1u << 22);
+                scales[c] = scale_of(byte);
                 if ((FM == 4 || wave < 2) && col0 + c < p.n && row0 < p.m)
                     e.y8.turned_scale[(col0 + c) * e.y8.turned_scale_ld + row0 / kFp8Block] = (uint8_t)byte;
             }
@@ -376,10 +375,10 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
                     for (int w = 0; w < 8; ++w) scale[w] = scales[c0 + w];
 #pragma unroll
                     for (int w = 0; w < 8; w += 4 / FM) {
-                        float x[4];
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) x[b] = sum[b % FM][j][8 * o + w + b / FM] * scale[w + b / FM];
-                        const uint32_t word = turn_bytes(four_e4m3(x[0], x[1], x[2], x[3], 1.0f), in);
+                        const auto at = [&](int b) { return sum[b % FM][j][8 * o + w + b / FM]; };
+                        i16x2 four = two_e4m3<0>(i16x2{0, 0}, at(0), at(1), scale[w]);
+                        four = two_e4m3<1>(four, at(2), at(3), scale[w + 2 / FM]);
+                        const uint32_t word = turn_bytes(__builtin_bit_cast(uint32_t, four), in);
                         const int kind = in & 3;
                         *reinterpret_cast<uint32_t*>(slot(c0 + w + kind / FM) + 32 * (kind % FM) + (in & ~3)) = word;
                     }

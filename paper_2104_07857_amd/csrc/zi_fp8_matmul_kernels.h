@@ -453,14 +453,14 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
 // Up to 16 FA rows of A: what counts is how fast B's rows come.  A workgroup has 16 of them, whose k its wavefronts share out in runs of four
 // blocks, W runs at a time, with all of a run's loads in flight at once and its four scales in a word; nothing passes through LDS but the
 // wavefronts' sums, which are added in their order.  1 x 4096 x 4096 4.8 us, 1 x 1024 x 1024 2.3.
-template <int DT, int FA, int W>
-__global__ __launch_bounds__(64 * W) void fp8_matmul_few_kernel(const MatmulArgs p)
+template <int FA, int W>
+using FewSums = float[W][FA][16][17];
+template <int FA, int W>
+__device__ __forceinline__ void multiply_few(const MatmulArgs& p, int64_t n0, FewSums<FA, W>& s_sum)
 {
     constexpr int kRun = 4;
-    __shared__ float s_sum[W][FA][16][17];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int in = lane & 15, part = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
     const int64_t row_b = n0 + in < p.n ? n0 + in : p.n - 1;
     const uint8_t* at_b = p.b + row_b * p.b_ld;
     const uint8_t* scale_b = p.b_scale + (row_b >> p.b_shift) * p.b_scale_ld;
@@ -516,13 +516,28 @@ __global__ __launch_bounds__(64 * W) void fp8_matmul_few_kernel(const MatmulArgs
 #pragma unroll
         for (int r = 0; r < 4; ++r) s_sum[wave][f][in][4 * part + r] = sum[f][r];
     __syncthreads();
+}
+// The sum of all wavefronts, in their order.
+template <int FA, int W>
+__device__ __forceinline__ float sum_of_few(const FewSums<FA, W>& s_sum, int f, int m, int n)
+{
+    float x = s_sum[0][f][m][n];
+#pragma unroll
+    for (int w = 1; w < W; ++w) x += s_sum[w][f][m][n];
+    return x;
+}
+
+template <int DT, int FA, int W>
+__global__ __launch_bounds__(64 * W) void fp8_matmul_few_kernel(const MatmulArgs p)
+{
+    __shared__ float s_sum[W][FA][16][17];
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    multiply_few<FA, W>(p, n0, s_sum);
     for (int i = threadIdx.x; i < FA * 256; i += 64 * W) {
         const int f = i >> 8, m = (i >> 4) & 15, n = i & 15;
         const int64_t row = 16 * f + m, col = n0 + n;
         if (row >= p.m || col >= p.n) continue;
-        float x = s_sum[0][f][m][n];
-#pragma unroll
-        for (int w = 1; w < W; ++w) x += s_sum[w][f][m][n];
+        float x = sum_of_few<FA, W>(s_sum, f, m, n);
         if constexpr (DT == ZI_FP32) {
             static_cast<float*>(p.d)[row * p.d_ld + col] = x;
         } else {
