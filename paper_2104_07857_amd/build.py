@@ -17,7 +17,8 @@ LIB_PATH = os.path.join(HERE, "libzi.so")
 CALL_PATH = os.path.join(HERE, "_zi_call" + importlib.machinery.EXTENSION_SUFFIXES[0])
 SOURCES = ["zi_kernels.hip", "zi_api.hip", "zi_plan.hip", "zi_engine.hip", "zi_offload.hip", "zi_probe.hip",
            "zi_fp8_api.hip", "zi_fp8_rows.hip", "zi_fp8_matmul.hip",
-           "zi_epilogue_api.hip", "zi_epilogue.hip", "zi_fp8_matmul_epilogue.hip",
+           "zi_epilogue_api.hip", "zi_epilogue_rows.hip", "zi_epilogue_tiles.hip", "zi_epilogue_backward.hip",
+           "zi_fp8_matmul_epilogue.hip",
            "zi_fp8_matmul_floor.hip", "zi_fp8_matmul_sigmoid.hip", "zi_fp8_matmul_normal.hip"]
 
 # -ffp-contract=off: the only fused multiply-adds are the ones the kernels write as fma.

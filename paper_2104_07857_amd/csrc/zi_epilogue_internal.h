@@ -24,7 +24,7 @@ struct EpilogueArgs {
     DropoutArgs drop;
     int32_t activation;
     QuantizeArgs y8;              // its out and turned; x and ld are not used
-    bool large;                   // outputs are streamed past the caches
+    bool large_out;               // outputs alone are more than what is worth keeping in the caches
 };
 // Where x comes from: 16 bits, or the sums that a product left in parts of rows x cols.
 struct EpilogueSource {
@@ -33,6 +33,7 @@ struct EpilogueSource {
     const float* sums;
     uint32_t parts;
 };
+hipError_t launch_epilogue_tiles(const EpilogueArgs& e, const EpilogueSource& x, int dtype, hipStream_t s);     // also where `turned` is wanted
 hipError_t launch_epilogue(const EpilogueArgs& e, const EpilogueSource& x, int dtype, hipStream_t s);
 
 size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int outputs8);
@@ -49,7 +50,7 @@ struct EpilogueBackwardArgs {
     DropoutArgs drop;
     int32_t activation;
     QuantizeArgs dz8;
-    bool large;
+    bool large_out;
 };
 hipError_t launch_epilogue_backward(const EpilogueBackwardArgs& a, int dtype, float* workspace, hipStream_t s);
 

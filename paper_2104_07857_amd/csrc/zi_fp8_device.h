@@ -30,7 +30,8 @@ struct Octet {
     uint32_t w[kWords];
 
     // The octet at `at`, of which a row of `cols` has `left` more elements (none or less than none: zeros); zeros behind its end.
-    template <Ends ENDS>
+    // STREAM: past the caches, of what is more than they hold.
+    template <Ends ENDS, bool STREAM = false>
     __device__ __forceinline__ void load(const void* base, int64_t at, int left)
     {
         int past = 0;
@@ -44,7 +45,9 @@ struct Octet {
         const char* p = static_cast<const char*>(base) + (at - past) * kBytes;
 #pragma unroll
         for (int i = 0; i < kWords / 4; ++i) {
-            const vec v = reinterpret_cast<const vec*>(p)[i];
+            vec v;
+            if constexpr (STREAM) v = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p) + i);
+            else v = reinterpret_cast<const vec*>(p)[i];
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
         }
