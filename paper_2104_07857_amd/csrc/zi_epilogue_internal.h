@@ -36,6 +36,11 @@ struct EpilogueSource {
 hipError_t launch_epilogue_tiles(const EpilogueArgs& e, const EpilogueSource& x, int dtype, hipStream_t s);     // also where `turned` is wanted
 hipError_t launch_epilogue(const EpilogueArgs& e, const EpilogueSource& x, int dtype, hipStream_t s);
 
+struct EpiloguePlan {
+    MatmulPlan plan;
+    int32_t whole;                // all outputs come from the product's kernel; else a second one makes them of its sums
+};
+EpiloguePlan plan_fp8_matmul_epilogue(int64_t m, int64_t n, int64_t k, int outputs8);
 size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int outputs8);
 hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpilogueArgs& e, int dtype, float* workspace, hipStream_t s);
 

@@ -12,8 +12,6 @@ hipError_t launch_fp8_matmul_epilogue_tiles<ActivationKind::kSigmoid>(const Matm
 template <>
 hipError_t launch_fp8_matmul_epilogue_tiles<ActivationKind::kNormal>(const MatmulArgs&, const MatmulPlan&, const EpilogueArgs&, int, hipStream_t);
 
-namespace {
-
 // Few rows, whose sums become 16-bit outputs here, element by element.  (Of eight numbers that dropout's generator makes at a time one is used; blocks of 128 columns are eight
 // workgroups', so that outputs in 8 bits are left to a second kernel.)
 template <int DT, int FA, int W>
@@ -65,6 +63,8 @@ __global__ __launch_bounds__(64 * W) void fp8_matmul_few_epilogue_kernel(const M
         put(e.y, row * e.y_ld + col, x);
     }
 }
+namespace {
+
 template <int DT>
 hipError_t launch_few_epilogue(const MatmulArgs& a, const EpilogueArgs& e, hipStream_t s)
 {
@@ -72,26 +72,6 @@ hipError_t launch_few_epilogue(const MatmulArgs& a, const EpilogueArgs& e, hipSt
     if (a.m <= 16) hipLaunchKernelGGL((fp8_matmul_few_epilogue_kernel<DT, 1, 8>), grid, block, 0, s, a, e);
     else hipLaunchKernelGGL((fp8_matmul_few_epilogue_kernel<DT, 2, 8>), grid, block, 0, s, a, e);
     return hipGetLastError();
-}
-
-// How a product is made, and whether all of its outputs come from there: tiles put out blocks of 128 rows or columns that are a workgroup's own.  Where the fastest way to the sums is none
-// to the outputs, a second kernel that reads the sums again stands against the fastest way that is.
-struct EpiloguePlan {
-    MatmulPlan plan;
-    bool whole;
-};
-constexpr float kSecond = 2.5f, kSecondStream = 4.5e6f, kWhole = 1.5f;      // us of the second kernel; bytes a us; us of blocks made in tiles
-EpiloguePlan plan_epilogue(int64_t m, int64_t n, int64_t k, int outputs8)
-{
-    const int first = outputs8 & ZI_EPILOGUE_TURNED ? 2 : outputs8 & ZI_EPILOGUE_Y8 ? 1 : kFewRows;
-    float any, whole;
-    const MatmulPlan plan = plan_fp8_matmul_from(m, n, k, kFewRows, any);
-    if (plan.parts == 1 && plan.shape >= first) return {plan, true};
-    const MatmulPlan other = plan_fp8_matmul_from(m, n, k, first > 0 ? first : 0, whole);
-    // (The estimate for parts has their sum in it already.)  1 x 16384 x 4096 to 8 bits: in two kernels 15.0 us, whole in tiles of 64 x 128 17.3; 2048 x 2048 x 2048 transposed 22 and 14.
-    const float second = plan.parts > 1 ? 0.0f : kSecond + 8.0f * (float)m * (float)n / kSecondStream;
-    if (other.parts == 1 && whole + kWhole <= any + second) return {other, true};
-    return {plan, false};
 }
 
 // Sums in a workspace, for a kernel over rows or tiles to go on with.
@@ -119,15 +99,31 @@ hipError_t launch_sums(const MatmulArgs& a, const MatmulPlan& plan, float* sums,
 
 }  // namespace
 
+// How a product is made, and whether all of its outputs come from there: tiles put out blocks of 128 rows or columns that are a workgroup's own.  Where the fastest way to the sums is none
+// to the outputs, a second kernel that reads the sums again stands against the fastest way that is.
+static constexpr float kSecond = 2.5f, kSecondStream = 4.5e6f, kWhole = 1.5f;      // us of the second kernel; bytes a us; us of blocks made in tiles
+EpiloguePlan plan_fp8_matmul_epilogue(int64_t m, int64_t n, int64_t k, int outputs8)
+{
+    const int first = outputs8 & ZI_EPILOGUE_TURNED ? 2 : outputs8 & ZI_EPILOGUE_Y8 ? 1 : kFewRows;
+    float any, whole;
+    const MatmulPlan plan = plan_fp8_matmul_from(m, n, k, kFewRows, any);
+    if (plan.parts == 1 && plan.shape >= first) return {plan, 1};
+    const MatmulPlan other = plan_fp8_matmul_from(m, n, k, first > 0 ? first : 0, whole);
+    // (The estimate for parts has their sum in it already.)  1 x 16384 x 4096 to 8 bits: in two kernels 15.0 us, whole in tiles of 64 x 128 17.3; 2048 x 2048 x 2048 transposed 22 and 14.
+    const float second = plan.parts > 1 ? 0.0f : kSecond + 8.0f * (float)m * (float)n / kSecondStream;
+    if (other.parts == 1 && whole + kWhole <= any + second) return {other, 1};
+    return {plan, 0};
+}
+
 size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int outputs8)
 {
-    const EpiloguePlan p = plan_epilogue(m, n, k, outputs8);
+    const EpiloguePlan p = plan_fp8_matmul_epilogue(m, n, k, outputs8);
     return p.whole ? 0 : p.plan.parts * (size_t)m * (size_t)n;
 }
 
 hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpilogueArgs& e, int dtype, float* workspace, hipStream_t s)
 {
-    const EpiloguePlan p = plan_epilogue(a.m, a.n, a.k, (e.y8.out ? ZI_EPILOGUE_Y8 : 0) | (e.y8.turned ? ZI_EPILOGUE_TURNED : 0));
+    const EpiloguePlan p = plan_fp8_matmul_epilogue(a.m, a.n, a.k, (e.y8.out ? ZI_EPILOGUE_Y8 : 0) | (e.y8.turned ? ZI_EPILOGUE_TURNED : 0));
     if (!p.whole) {
         const hipError_t err = launch_sums(a, p.plan, workspace, s);
         if (err != hipSuccess) return err;

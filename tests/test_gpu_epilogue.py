@@ -334,3 +334,31 @@ def test_matrices_of_more_than_four_gib():
         assert torch.equal(dz[r:r + 1].double(), want)
         total += want[0]
     assert torch.equal(dbias.double(), total)
+
+
+@pytest.mark.parametrize("cols", [8200, 8203])
+@pytest.mark.parametrize("activation", list(ACTIVATIONS))
+def test_large_calls_are_like_small_ones(cols, activation):
+    """What is read and written past the caches: the same bits as of its rows by 1280 at a time, whose calls are small.  (The mask goes by the row, so nothing is dropped.)"""
+    rows, part = 16640, 1280                                              # 136 million elements, 546 MB and more
+    dtype = torch.float16 if cols % 8 else torch.bfloat16
+    x, residual, bias = normal((rows, cols), 40, 2.0, dtype), normal((rows, cols), 41, 1.0, dtype), normal((cols,), 42, 0.5, dtype)
+    for outputs, r in (("z,y,y8", residual), ("y,y8,turned", None)):
+        a = Forward(x, activation, outputs, bias, r)
+        for at in range(0, rows, part):
+            rest = slice(at, at + part)
+            b = Forward(x[rest], activation, outputs, bias, None if r is None else r[rest])
+            assert torch.equal(a.y[rest], b.y) and (a.z is None or torch.equal(a.z[rest], b.z))
+            assert torch.equal(a.y8.codes()[rest], b.y8.codes()) and torch.equal(a.y8.scales()[rest], b.y8.scales())
+            if a.turned:
+                assert torch.equal(a.turned.codes()[:, rest], b.turned.codes()) and torch.equal(a.turned.scales()[:, at // 128:(at + part) // 128], b.turned.scales())
+    dbias, total = torch.empty(cols, device="cuda:0"), torch.zeros(cols, dtype=torch.float64, device="cuda:0")
+    a = Backward(residual, x, activation, "dz,dz8,turned", dbias=dbias)
+    for at in range(0, rows, part):
+        rest = slice(at, at + part)
+        b = Backward(residual[rest], x[rest], activation, "dz,dz8,turned", dbias=torch.empty(cols, device="cuda:0"))
+        assert torch.equal(a.dz[rest], b.dz) and torch.equal(a.dz8.codes()[rest], b.dz8.codes()) and torch.equal(a.turned.codes()[:, rest], b.turned.codes())
+        total += b.dbias.double()
+    # each of 13 sums and their total: 160 additions and less follow each other
+    size = a.dz.double().abs().sum(0)
+    assert bool(((dbias.double() - total).abs() <= size * 320 * 2.0 ** -24).all())

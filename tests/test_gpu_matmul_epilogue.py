@@ -1,10 +1,11 @@
-"""zi_fp8_matmul_epilogue against the product in 64 bits and what follows it.  Whole numbers are exact, as test_gpu_fp8_matmul.py explains, through every kernel (the sizes of fp8_plans.py);
+"""zi_fp8_matmul_epilogue against the product in 64 bits and what follows it.  Whole numbers are exact, as test_gpu_fp8_matmul.py explains, through every kernel (test_epilogue_plans.py says that these sizes reach them);
 normal numbers meet the matrix cores' own bound that it derives, on top of that of epilogue_util.py."""
 import pytest
 import torch
 
 import paper_2104_07857_amd as zi
 from epilogue_util import ACTIVATIONS, OFFSET, SEED, act, dropped, factor, kept, near, near8, same8
+from epilogue_plans import SUMS
 from fp8_plans import FEW_16, FEW_32, PARTS, TILES
 from fp8_util import DT, Matrix, normal, numbers, quantized, same, view_of
 from test_gpu_epilogue import _empty, _is_quantised, _whole
@@ -60,7 +61,7 @@ def _want(product, activation, drop, bias, residual):
     return z, y if residual is None else y + residual.double()
 
 
-ALL = FEW_16 + FEW_32 + PARTS + TILES
+ALL = FEW_16 + FEW_32 + PARTS + TILES + SUMS
 
 
 @pytest.mark.parametrize("m,n,k", ALL)
@@ -124,6 +125,23 @@ def test_nan_keeps_to_its_place(m, n, k):
     assert same(p.y8.values().isnan().double(), y.isnan().double()) and same(p.turned.values().t().isnan().double(), y.isnan().double())
     codes, scales = quantized(y, 1)
     assert torch.equal(p.y8.scales(), scales) and same(numbers(p.y8.codes()), codes)
+
+
+@pytest.mark.parametrize("m,n,k", [FEW_16[3], PARTS[1], TILES[3], TILES[7], TILES[8], TILES[9], TILES[11], TILES[12], TILES[16]])
+def test_infinities_have_no_part_in_a_scale(m, n, k):
+    """A row of A whose products pass what fp32 holds: infinities in its row of y, NaN in 8 bits, and the scales of its columns' blocks those of the other rows."""
+    a, b = _whole8(m, k, 1, 20), _whole8(n, k, 1, 21)
+    b.data[:, 0], a.data[m // 2] = 0x38, 0
+    a.data[m // 2, 0], a.scale[m // 2, 0] = 0x7E, 254                     # 448 * 2^127
+    product = _exact(a, b)
+    y = torch.where(product.abs() > 2.0 ** 128, torch.full_like(product, float("inf")), product)
+    assert bool(y[m // 2].isinf().all()) and int(y.isinf().sum()) == n
+    p = Product(a, b, torch.bfloat16, "relu", "y,y8,turned")
+    want = y.clamp_min(0)
+    assert torch.equal(p.y.double(), want.to(torch.bfloat16).double())
+    for matrix, value in ((p.y8, want), (p.turned, want.t())):
+        codes, scales = quantized(value, 1)
+        assert torch.equal(matrix.scales(), scales) and same(numbers(matrix.codes()), codes)
 
 
 @pytest.mark.parametrize("m,n", [(1, 5), (40, 300), (300, 700), (2100, 2200)])
