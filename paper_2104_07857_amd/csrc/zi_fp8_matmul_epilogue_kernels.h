@@ -132,12 +132,16 @@ __device__ __forceinline__ uint32_t turn_bytes(uint32_t w, int in)
     return __builtin_amdgcn_perm(b, w, in & 2 ? 0x03020706u : 0x05040100u);
 }
 
+// What a kernel is made for: z and y in 16 bits; outputs in 8 bits (and y), with z or without.
+enum class TileOutputs { k16, k8, k8AndZ };
+
 // Tiles as fp8_matmul_kernel has them, and what follows the product while its sums are in registers.  A wavefront's sums turn to rows in LDS for z, the residual and y; what is quantised stays
 // in fp32 registers until its blocks' scales are known, which wavefronts side by side (FN 2) or below each other (FM 2) find together.
-template <int DT, int FM, int FN, int RING, bool EIGHTS, ActivationKind KIND>
+template <int DT, int FM, int FN, int RING, TileOutputs OUTPUTS, ActivationKind KIND>
 __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_epilogue_kernel(const MatmulArgs p, const TileOrder order, const EpilogueArgs e)
 {
     constexpr int kM = 64 * FM, kN = 64 * FN, kStage = (kM + kN) * kStep;
+    constexpr bool EIGHTS = OUTPUTS != TileOutputs::k16, Z = OUTPUTS == TileOutputs::k8AndZ;
     __shared__ __align__(128) uint8_t s_stage[RING * kStage];
     __shared__ __align__(128) uint32_t s_scale[2 * (kM + kN)];
     __shared__ __align__(16) uint16_t s_bias[kN];
@@ -193,20 +197,26 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
         w.set(x);
         *reinterpret_cast<u32x4*>(rows.chunk(32 * i + in, 4 * j + 2 * o + half)) = u32x4{w.w[0], w.w[1], w.w[2], w.w[3]};
     };
-    if (e.z) {
+    // (Where y stays in registers, z is there first by itself, whether it goes out or not: both at once take more registers than there are.)
+    if (EIGHTS || e.z) {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 const f32x16 z = with_bias(sum[i][j], j);
+                if constexpr (EIGHTS) sum[i][j] = z;
+                if constexpr (Z || !EIGHTS) {
 #pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                    float x[8];
+                    for (int o = 0; o < 2; ++o) {
+                        float x[8];
 #pragma unroll
-                    for (int w = 0; w < 8; ++w) x[w] = z[8 * o + w];
-                    put(x, i, j, o);
+                        for (int w = 0; w < 8; ++w) x[w] = z[8 * o + w];
+                        put(x, i, j, o);
+                    }
                 }
             }
+    }
+    if (EIGHTS ? Z : e.z != nullptr) {
         lanes_meet();
         rows.to_memory(e.z, e.z_ld);
         lanes_meet();
@@ -216,12 +226,16 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
         rows.from_memory(e.residual, e.residual_ld);
         lanes_meet();
     }
+    float row_most[FM];
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const int64_t row = row0 + 32 * i + in;
+        row_most[i] = 0.0f;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const f32x16 z = with_bias(sum[i][j], j);
+            f32x16 z;
+            if constexpr (EIGHTS) z = sum[i][j];
+            else z = with_bias(sum[i][j], j);
             float y[2][8];
 #pragma unroll
             for (int w = 0; w < 16; ++w) y[w / 8][w % 8] = activated_as<KIND>(form, z[w]);
@@ -252,6 +266,8 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
                 }
 #pragma unroll
                 for (int w = 0; w < 16; ++w) sum[i][j][w] = y[w / 8][w % 8];
+#pragma unroll
+                for (int w = 0; w < 16; w += 2) row_most[i] = larger<false>(y[w / 8][w % 8], y[w / 8][w % 8 + 1], row_most[i]);
             }
         }
     }
@@ -264,21 +280,21 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
         if (e.y8.out) {
             // A row's block of 128 columns is the wavefront's own (FN 4), or half of it is its neighbour's.
             uint32_t most[FM];
-            const auto look = [&](auto finite) {
-                bool found = false;
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) found |= row_most[i] == __builtin_inff();
+            if (__any(found)) {                         // an infinity: the largest without it
 #pragma unroll
                 for (int i = 0; i < FM; ++i) {
-                    float m = 0.0f;
+                    row_most[i] = 0.0f;
 #pragma unroll
                     for (int j = 0; j < FN; ++j)
 #pragma unroll
-                        for (int w = 0; w < 16; w += 2) m = larger<decltype(finite)::value>(sum[i][j][w], sum[i][j][w + 1], m);
-                    most[i] = __float_as_uint(m);
-                    found |= m == __builtin_inff();
+                        for (int w = 0; w < 16; w += 2) row_most[i] = larger<true>(sum[i][j][w], sum[i][j][w + 1], row_most[i]);
                 }
-                return found;
-            };
-            if (__any(look(std::false_type()))) look(std::true_type());
+            }
+#pragma unroll
+            for (int i = 0; i < FM; ++i) most[i] = __float_as_uint(row_most[i]);
 #pragma unroll
             for (int i = 0; i < FM; ++i) most[i] = max_of(most[i], (uint32_t)__shfl_xor((int)most[i], 32));
             if constexpr (FN == 2) {
@@ -310,12 +326,20 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
             const int own_row = lane / kChunks8, own_chunk = lane % kChunks8;
             const int64_t col = col0 + own_chunk * 16;
             uint8_t* at = e.y8.out + (row0 + own_row) * e.y8.out_ld + col;
-#pragma unroll 8
-            for (int r = own_row; r < 32 * FM; r += kAtOnce8, at += kAtOnce8 * e.y8.out_ld) {
-                if (row0 + r >= p.m || col >= p.n) continue;
-                const u32x4 x = *reinterpret_cast<const u32x4*>(chunk8(r, own_chunk));
-                if (p.n - col > 8) *reinterpret_cast<u32x4*>(at) = x;
-                else *reinterpret_cast<u32x2*>(at) = u32x2{x[0], x[1]};
+            if (rows.inside) {
+                constexpr int kTurns = 32 * FM / kAtOnce8;
+                u32x4 x[kTurns];
+#pragma unroll
+                for (int i = 0; i < kTurns; ++i) x[i] = *reinterpret_cast<const u32x4*>(chunk8(own_row + i * kAtOnce8, own_chunk));
+#pragma unroll
+                for (int i = 0; i < kTurns; ++i, at += kAtOnce8 * e.y8.out_ld) *reinterpret_cast<u32x4*>(at) = x[i];
+            } else {
+                for (int r = own_row; r < 32 * FM; r += kAtOnce8, at += kAtOnce8 * e.y8.out_ld) {
+                    if (row0 + r >= p.m || col >= p.n) continue;
+                    const u32x4 x = *reinterpret_cast<const u32x4*>(chunk8(r, own_chunk));
+                    if (p.n - col > 8) *reinterpret_cast<u32x4*>(at) = x;
+                    else *reinterpret_cast<u32x2*>(at) = u32x2{x[0], x[1]};
+                }
             }
             lanes_meet();
         }
@@ -388,10 +412,18 @@ __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_
             const int own_chunk = lane % kChunksDown, own_col = lane / kChunksDown;
             const int64_t row = row0 + own_chunk * 16;
             uint8_t* at = e.y8.turned + (col0 + own_col) * e.y8.turned_ld + row;
-#pragma unroll 8
-            for (int c = own_col; c < 32 * FN; c += kColsAtOnce, at += kColsAtOnce * e.y8.turned_ld) {
-                if (row >= p.m || col0 + c >= p.n) continue;
-                *reinterpret_cast<u32x4*>(at) = *reinterpret_cast<const u32x4*>(slot(c) + own_chunk * 16);
+            if (rows.inside) {
+                constexpr int kTurns = 32 * FN / kColsAtOnce;
+                u32x4 x[kTurns];
+#pragma unroll
+                for (int i = 0; i < kTurns; ++i) x[i] = *reinterpret_cast<const u32x4*>(slot(own_col + i * kColsAtOnce) + own_chunk * 16);
+#pragma unroll
+                for (int i = 0; i < kTurns; ++i, at += kColsAtOnce * e.y8.turned_ld) *reinterpret_cast<u32x4*>(at) = x[i];
+            } else {
+                for (int c = own_col; c < 32 * FN; c += kColsAtOnce, at += kColsAtOnce * e.y8.turned_ld) {
+                    if (row >= p.m || col0 + c >= p.n) continue;
+                    *reinterpret_cast<u32x4*>(at) = *reinterpret_cast<const u32x4*>(slot(c) + own_chunk * 16);
+                }
             }
         }
     }
@@ -411,8 +443,14 @@ template <ActivationKind KIND, int DT, int FM, int FN, int RING>
 hipError_t launch_epilogue_tiles(const MatmulArgs& a, const MatmulPlan& plan, const EpilogueArgs& e, hipStream_t s)
 {
     const TileOrder order = order_of(a, plan, 64 * FM, 64 * FN);
-    if (!e.y8.out && !e.y8.turned) hipLaunchKernelGGL((fp8_matmul_epilogue_kernel<DT, FM, FN, RING, false, KIND>), dim3(order.count), dim3(256), 0, s, a, order, e);
-    else if constexpr (FN >= 2) hipLaunchKernelGGL((fp8_matmul_epilogue_kernel<DT, FM, FN, RING, true, KIND>), dim3(order.count), dim3(256), 0, s, a, order, e);
+    const auto launch = [&](auto outputs) {
+        hipLaunchKernelGGL((fp8_matmul_epilogue_kernel<DT, FM, FN, RING, decltype(outputs)::value, KIND>), dim3(order.count), dim3(256), 0, s, a, order, e);
+    };
+    if (!e.y8.out && !e.y8.turned) launch(std::integral_constant<TileOutputs, TileOutputs::k16>());
+    else if constexpr (FN >= 2) {
+        if (e.z) launch(std::integral_constant<TileOutputs, TileOutputs::k8AndZ>());
+        else launch(std::integral_constant<TileOutputs, TileOutputs::k8>());
+    }
     return hipGetLastError();
 }
 template <ActivationKind KIND, int DT>
