@@ -336,6 +336,20 @@ def test_matrices_of_more_than_four_gib():
     assert torch.equal(dbias.double(), total)
 
 
+@pytest.mark.parametrize("rows,cols", [(2 ** 25 + 37, 3), (2 ** 24 + 21, 136)])
+def test_more_rows_than_are_under_way_at_a_time(rows, cols):
+    """A launch has 2^20 workgroups at most, which then go on to further rows (of 32 and of 16 each)."""
+    x = (torch.arange(rows, device="cuda:0", dtype=torch.int32)[:, None] * 7 + torch.arange(cols, device="cuda:0", dtype=torch.int32)).remainder_(255).sub_(127).to(torch.bfloat16)
+    y = torch.full_like(x, float("nan"))
+    zi.zi_epilogue(x, rows, cols, cols, zi.make_epilogue(rows, cols, zi.ZI_BF16, y=y, activation=zi.ZI_ACT_RELU))
+    torch.cuda.synchronize()
+    assert torch.equal(y, x.clamp_min(0))
+    zi.zi_epilogue(x, rows, cols, cols, zi.make_epilogue(rows, cols, zi.ZI_BF16, y=y, drop=0.5, seed=SEED, offset=OFFSET))
+    torch.cuda.synchronize()
+    for r in (0, rows - 40, rows - 3):
+        assert torch.equal(y[r:r + 3].double(), forward(x[r:r + 3], "none", 0.5, row0=r)[1])
+
+
 @pytest.mark.parametrize("cols", [8200, 8203])
 @pytest.mark.parametrize("activation", list(ACTIVATIONS))
 def test_large_calls_are_like_small_ones(cols, activation):
