@@ -3,7 +3,9 @@
 
 namespace zi {
 
-// Rows as they are.  L lanes have a strip of 8 L columns, whose bias stays in registers, and R rows each at a time, whose loads go out together.
+// Rows as they are, for what has no transposed output.  Bound by memory: all is read and written once.  L lanes have a strip of 8 L columns, and R rows each at a time, whose loads go out together;
+// narrow matrices' rows are side by side in a wavefront (L 16), so that its lanes are not idle.  A block's scale is a maximum over 16 lanes.  Dropout makes eight numbers at a time, 73 vector
+// instructions an octet, which 6 TB/s leave room for.  Dropout and residual of 16384 x 4096 63 us (403 MB, 6.4 TB/s); 333 x 1000 4.6; one row of 16384 to 8 bits with GELU 3.8, and of sums 2.9.
 template <int DT, int ACT, bool SUMS, int L, int R, Ends ENDS, bool LARGE>
 __global__ __launch_bounds__(256) void epilogue_rows_kernel(const EpilogueArgs e, const EpilogueSource from, uint32_t strips)
 {

@@ -3,7 +3,8 @@
 
 namespace zi {
 
-// Tiles, whose transposed numbers are wanted.
+// Tiles of 128 x 128, where transposed numbers are wanted: both directions' blocks are in one workgroup, x is read once.  Bound by memory, with the vector units close behind (13.6 instructions an
+// element for SiLU and both outputs).  8192 x 16384 to 8 bits both ways 104 us (539 MB, 5.2 TB/s; a rectangle of 128 bytes in every row and column is what an output gets at a time).
 template <int DT, int ACT, bool SUMS, Ends ENDS, bool LARGE>
 __global__ __launch_bounds__(256) void epilogue_tiles_kernel(const EpilogueArgs e, const EpilogueSource from)
 {

@@ -13,7 +13,8 @@ template <>
 hipError_t launch_fp8_matmul_epilogue_tiles<ActivationKind::kNormal>(const MatmulArgs&, const MatmulPlan&, const EpilogueArgs&, int, hipStream_t);
 
 // Few rows, whose sums become 16-bit outputs here, element by element.  (Of eight numbers that dropout's generator makes at a time one is used; blocks of 128 columns are eight
-// workgroups', so that outputs in 8 bits are left to a second kernel.)
+// workgroups', so that outputs in 8 bits are left to a second kernel.)  Bound by B's bytes; bias and residual come while they do.  us, fp8_matmul_few_kernel with C / this with bias, dropout
+// and residual: 1 x 4096 x 4096 4.9 / 5.5, 8 x 4096 x 4096 5.5 / 5.8, 24 x 4096 x 2048 7.4 / 8.3.
 template <int DT, int FA, int W>
 __global__ __launch_bounds__(64 * W) void fp8_matmul_few_epilogue_kernel(const MatmulArgs p, const EpilogueArgs e)
 {
@@ -121,6 +122,25 @@ size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int
     return p.whole ? 0 : p.plan.parts * (size_t)m * (size_t)n;
 }
 
+// Tiles of 256 rows leave a compute unit to one workgroup, and nothing beside it hides what becomes of its sums: that is cheaper in a kernel over tiles that reads z again, where z goes out
+// and y does not (which would else be rounded twice; what is in 8 bits is rounded 16 times as far).  us, one kernel / two, 8 bits both ways: with gelu 8191 x 8192 x 2048 252 / 192,
+// 4096 x 16384 x 4096 339 / 277, 8192 x 32768 x 8192 2026 / 1815, without an activation 203 / 172, 293 / 262, 1855 / 1755; one way with gelu 4096 x 16384 x 4096 310 / 265, without 254 / 254.
+// In smaller tiles, of which a compute unit has two, one kernel it is: 1001 x 8192 x 2048 30 / 34, 4096 x 4096 x 1024 40 / 45, 6000 x 12000 x 512 120 / 127.
+constexpr int kAlone = 4;      // the shapes from here on
+static hipError_t launch_z_first(const MatmulArgs& a, const MatmulPlan& plan, const EpilogueArgs& e, int dtype, hipStream_t s)
+{
+    EpilogueArgs first = e, then = e;
+    first.residual = nullptr;
+    first.drop = DropoutArgs{};
+    first.activation = ZI_ACT_NONE;
+    first.y8 = QuantizeArgs{};
+    const hipError_t err = launch_fp8_matmul_epilogue_tiles<ActivationKind::kFloor>(a, plan, first, dtype, s);
+    if (err != hipSuccess) return err;
+    then.bias = nullptr;
+    then.z = nullptr;
+    return launch_epilogue(then, EpilogueSource{e.z, e.z_ld, nullptr, 0}, dtype, s);
+}
+
 hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpilogueArgs& e, int dtype, float* workspace, hipStream_t s)
 {
     const EpiloguePlan p = plan_fp8_matmul_epilogue(a.m, a.n, a.k, (e.y8.out ? ZI_EPILOGUE_Y8 : 0) | (e.y8.turned ? ZI_EPILOGUE_TURNED : 0));
@@ -129,6 +149,7 @@ hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpilogueArgs& e
         if (err != hipSuccess) return err;
         return launch_epilogue(e, EpilogueSource{nullptr, 0, workspace, p.plan.parts}, dtype, s);
     }
+    if (p.plan.shape >= kAlone && e.z && !e.y && (e.y8.out || e.y8.turned)) return launch_z_first(a, p.plan, e, dtype, s);
     if (p.plan.shape == kFewRows) return dtype == ZI_BF16 ? launch_few_epilogue<ZI_BF16>(a, e, s) : launch_few_epilogue<ZI_FP16>(a, e, s);
     switch (kind_of(e.activation)) {
     case ActivationKind::kFloor: return launch_fp8_matmul_epilogue_tiles<ActivationKind::kFloor>(a, p.plan, e, dtype, s);

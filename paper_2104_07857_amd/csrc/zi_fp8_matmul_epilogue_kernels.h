@@ -136,7 +136,9 @@ __device__ __forceinline__ uint32_t turn_bytes(uint32_t w, int in)
 enum class TileOutputs { k16, k8, k8AndZ };
 
 // Tiles as fp8_matmul_kernel has them, and what follows the product while its sums are in registers.  A wavefront's sums turn to rows in LDS for z, the residual and y; what is quantised stays
-// in fp32 registers until its blocks' scales are known, which wavefronts side by side (FN 2) or below each other (FM 2) find together.
+// in fp32 registers until its blocks' scales are known, which wavefronts side by side (FN 2) or below each other (FM 2) find together.  The product is the bound, and the epilogue what
+// nothing hides: with 256 x 256 in registers a compute unit has one workgroup.  us, product in 16 bits alone / y in 8 bits / bias, SiLU and y in 8 bits: 8192 x 32768 x 8192 1640 / 1650 /
+// 1748, 1001 x 8192 x 2048 (128 x 128, two on a compute unit) 20 / 22.7 / 24.  8191 x 4096 x 16384 with bias, dropout and residual 456; with C alone 430 to 450.
 template <int DT, int FM, int FN, int RING, TileOutputs OUTPUTS, ActivationKind KIND>
 __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_epilogue_kernel(const MatmulArgs p, const TileOrder order, const EpilogueArgs e)
 {

@@ -16,5 +16,13 @@ def plan(m, n, k, outputs8):
     return f(m, n, k, outputs8)
 
 
+def of_rounded_z(m, n, k, outputs):
+    """Whether outputs in 8 bits are made of z as it was written, by a second kernel: of tiles of 256 rows, where y is not wanted in 16 bits."""
+    wanted = outputs.split(",")
+    outputs8 = ("y8" in wanted) * Y8 + ("turned" in wanted) * TURNED
+    p = plan(m, n, k, outputs8)
+    return "z" in wanted and "y" not in wanted and outputs8 > 0 and p.whole == 1 and p.shape >= 4
+
+
 # sums of tiles of 64 x 128, of which a second kernel makes the transposed numbers
 SUMS = [(320, 6050, 8001), (300, 5003, 6100)]
