@@ -56,8 +56,13 @@ struct MatmulPlan {
 };
 constexpr int kFewRows = -1;
 MatmulPlan plan_fp8_matmul(int64_t m, int64_t n, int64_t k);
-// The same among shapes from `first` on, of which more than the smallest come in one part; and the time that it is expected to take, in us.
-MatmulPlan plan_fp8_matmul_from(int64_t m, int64_t n, int64_t k, int first, float& estimate);
+// The same among shapes from `first` on, of which more than the smallest come in one part; and the time that it is expected to take, in us.  `alone`: what an epilogue adds to a round of tiles of
+// 256 x 128 and of 256 x 256, which have a compute unit to themselves.
+struct MatmulAlone {
+    float rows_256_128, rows_256_256;
+};
+constexpr int kAloneShape = 4;       // the first of the two
+MatmulPlan plan_fp8_matmul_from(int64_t m, int64_t n, int64_t k, int first, const MatmulAlone& alone, float& estimate);
 hipError_t launch_fp8_matmul(const MatmulArgs& a, int dtype, float* partials, hipStream_t s);
 
 }  // namespace zi

@@ -95,9 +95,9 @@ static float few_rows_estimate(int64_t m, int64_t n, int64_t k)
 MatmulPlan plan_fp8_matmul(int64_t m, int64_t n, int64_t k)
 {
     float estimate;
-    return plan_fp8_matmul_from(m, n, k, kFewRows, estimate);
+    return plan_fp8_matmul_from(m, n, k, kFewRows, MatmulAlone{}, estimate);
 }
-MatmulPlan plan_fp8_matmul_from(int64_t m, int64_t n, int64_t k, int first, float& least)
+MatmulPlan plan_fp8_matmul_from(int64_t m, int64_t n, int64_t k, int first, const MatmulAlone& alone, float& least)
 {
     const int64_t steps = (k + kStep - 1) / kStep;
     const float stream = ((float)m + (float)n) * (float)k + kOutput * (float)m * (float)n;
@@ -106,12 +106,13 @@ MatmulPlan plan_fp8_matmul_from(int64_t m, int64_t n, int64_t k, int first, floa
     if (m <= 32 && first == kFewRows) least = few_rows_estimate(m, n, k);
     for (int i = first > 0 ? first : 0; i < kShapes; ++i) {
         const TileShape& t = kShape[i];
+        const float besides = t.besides + (i == kAloneShape ? alone.rows_256_128 : i == kAloneShape + 1 ? alone.rows_256_256 : 0.0f);
         const int64_t tiles = ((m + t.rows - 1) / t.rows) * ((n + t.cols - 1) / t.cols);
         for (int64_t parts = 1; parts <= (i == 0 ? 16 : 1); parts *= 2) {
             const int64_t each = ((steps + parts - 1) / parts + 3) / 4 * 4;       // a part begins with a word of scales
             const int64_t really = each ? (steps + each - 1) / each : 1;
             const int64_t groups = tiles * really, rounds = groups / (kUnits * t.together), rest = groups % (kUnits * t.together);
-            const auto round = [&](float step) { return (float)(really > 1 ? each : steps) * step + t.besides; };
+            const auto round = [&](float step) { return (float)(really > 1 ? each : steps) * step + besides; };
             const bool apart = t.together == 2 ? rest <= kUnits : rounds == 0 && rest <= kUnits / 2;
             const float work = (float)rounds * round(t.step_together) + (rest ? round(apart ? t.step : t.step_together) : 0.0f);
             float all = 0.01f * work + (work > stream / kStream ? work : stream / kStream);

@@ -102,18 +102,44 @@ hipError_t launch_sums(const MatmulArgs& a, const MatmulPlan& plan, float* sums,
 
 // How a product is made, and whether all of its outputs come from there: tiles put out blocks of 128 rows or columns that are a workgroup's own.  Where the fastest way to the sums is none
 // to the outputs, a second kernel that reads the sums again stands against the fastest way that is.
+//
+// Tiles of 256 rows have a compute unit to themselves, and nothing hides what becomes of their sums; of 128 x 128 there are two, one of which multiplies meanwhile.  So they are the faster ones for
+// outputs in 8 bits up to k of 4000 or so.  us, 256 x 256 / 128 x 128: 8191 x 8192 x 2048 with gelu to 8 bits 201 / 160, both ways 223 / 178, 4096 x 16384 x 4096 285 / 265 and 308 / 278,
+// 8192 x 32768 x 8192 1830 / 1967 and 1920 / 2055.  kAlone are fitted to 90 products (m of 64 to 16384, n of 128 to 32768, k of 181 to 16384, drawn evenly on a logarithmic scale) with outputs one way and both, without
+// an activation, with gelu and silu, in each tile: the choice is 0.2 % slower than the fastest tile for one way along the rows and 0.3 % for the others; without them 2.6 and 3.3 to 3.9 %.
 static constexpr float kSecond = 2.5f, kSecondStream = 4.5e6f, kWhole = 1.5f;      // us of the second kernel; bytes a us; us of blocks made in tiles
+static constexpr MatmulAlone kAloneRows = {8.0f, 8.0f}, kAloneTurned = {8.0f, 14.0f};      // us a round: outputs along the rows, and transposed
+static MatmulPlan plan_whole(int64_t m, int64_t n, int64_t k, int outputs8, float& estimate)
+{
+    const int first = outputs8 & ZI_EPILOGUE_TURNED ? 2 : outputs8 & ZI_EPILOGUE_Y8 ? 1 : 0;
+    return plan_fp8_matmul_from(m, n, k, first, outputs8 & ZI_EPILOGUE_TURNED ? kAloneTurned : outputs8 ? kAloneRows : MatmulAlone{}, estimate);
+}
 EpiloguePlan plan_fp8_matmul_epilogue(int64_t m, int64_t n, int64_t k, int outputs8)
 {
     const int first = outputs8 & ZI_EPILOGUE_TURNED ? 2 : outputs8 & ZI_EPILOGUE_Y8 ? 1 : kFewRows;
     float any, whole;
-    const MatmulPlan plan = plan_fp8_matmul_from(m, n, k, kFewRows, any);
-    if (plan.parts == 1 && plan.shape >= first) return {plan, 1};
-    const MatmulPlan other = plan_fp8_matmul_from(m, n, k, first > 0 ? first : 0, whole);
+    const MatmulPlan plan = plan_fp8_matmul_from(m, n, k, kFewRows, MatmulAlone{}, any);
+    if (outputs8 == 0 && plan.parts == 1) return {plan, 1};
+    const MatmulPlan other = plan_whole(m, n, k, outputs8, whole);
+    if (plan.parts == 1 && plan.shape >= first) return {other, 1};
     // (The estimate for parts has their sum in it already.)  1 x 16384 x 4096 to 8 bits: in two kernels 15.0 us, whole in tiles of 64 x 128 17.3; 2048 x 2048 x 2048 transposed 22 and 14.
     const float second = plan.parts > 1 ? 0.0f : kSecond + 8.0f * (float)m * (float)n / kSecondStream;
     if (other.parts == 1 && whole + kWhole <= any + second) return {other, 1};
     return {plan, 0};
+}
+
+// Where z goes out and y does not in 16 bits (which would else be rounded twice; what is in 8 bits is rounded 16 times as far), large products leave z first, in the fastest tiles for that, and what
+// is in 8 bits is made of it by a kernel that reads it again.  us, one kernel in 128 x 128 / two, with gelu, 8 bits both ways: 8191 x 8192 x 2048 194 / 175, 4096 x 16384 x 4096 306 / 259, 8192 x
+// 32768 x 8192 2175 / 1758 (in 256 x 256 252, 339 and 2026), without an activation 175 / 164, 285 / 250, 2084 / 1728; but 2048 x 8192 x 2048 49 / 52, and to 8 bits along the rows 39 / 45
+// without an activation and 1500 x 16384 x 4096 101 / 105.
+static constexpr float kZOut = 0.2e-6f, kZStream = 7.5e6f;       // us an element that z takes beside each of the others; bytes a us of the second kernel, which finds some of z in the caches
+bool fp8_matmul_z_first(int64_t m, int64_t n, int64_t k, int outputs8)
+{
+    float any, whole;
+    if (plan_fp8_matmul_from(m, n, k, kFewRows, MatmulAlone{}, any).shape < kAloneShape) return false;
+    plan_whole(m, n, k, outputs8, whole);
+    const float cells = (float)m * (float)n, out = (outputs8 & ZI_EPILOGUE_Y8 ? 1.0f : 0.0f) + (outputs8 & ZI_EPILOGUE_TURNED ? 1.0f : 0.0f);
+    return any + kSecond + (2.0f + out) * cells / kZStream < whole + kZOut * out * cells;
 }
 
 size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int outputs8)
@@ -122,19 +148,14 @@ size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int
     return p.whole ? 0 : p.plan.parts * (size_t)m * (size_t)n;
 }
 
-// Tiles of 256 rows leave a compute unit to one workgroup, and nothing beside it hides what becomes of its sums: that is cheaper in a kernel over tiles that reads z again, where z goes out
-// and y does not (which would else be rounded twice; what is in 8 bits is rounded 16 times as far).  us, one kernel / two, 8 bits both ways: with gelu 8191 x 8192 x 2048 252 / 192,
-// 4096 x 16384 x 4096 339 / 277, 8192 x 32768 x 8192 2026 / 1815, without an activation 203 / 172, 293 / 262, 1855 / 1755; one way with gelu 4096 x 16384 x 4096 310 / 265, without 254 / 254.
-// In smaller tiles, of which a compute unit has two, one kernel it is: 1001 x 8192 x 2048 30 / 34, 4096 x 4096 x 1024 40 / 45, 6000 x 12000 x 512 120 / 127.
-constexpr int kAlone = 4;      // the shapes from here on
-static hipError_t launch_z_first(const MatmulArgs& a, const MatmulPlan& plan, const EpilogueArgs& e, int dtype, hipStream_t s)
+static hipError_t launch_z_first(const MatmulArgs& a, const EpilogueArgs& e, int dtype, hipStream_t s)
 {
     EpilogueArgs first = e, then = e;
     first.residual = nullptr;
     first.drop = DropoutArgs{};
     first.activation = ZI_ACT_NONE;
     first.y8 = QuantizeArgs{};
-    const hipError_t err = launch_fp8_matmul_epilogue_tiles<ActivationKind::kFloor>(a, plan, first, dtype, s);
+    const hipError_t err = launch_fp8_matmul_epilogue_tiles<ActivationKind::kFloor>(a, plan_fp8_matmul(a.m, a.n, a.k), first, dtype, s);
     if (err != hipSuccess) return err;
     then.bias = nullptr;
     then.z = nullptr;
@@ -143,13 +164,14 @@ static hipError_t launch_z_first(const MatmulArgs& a, const MatmulPlan& plan, co
 
 hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpilogueArgs& e, int dtype, float* workspace, hipStream_t s)
 {
-    const EpiloguePlan p = plan_fp8_matmul_epilogue(a.m, a.n, a.k, (e.y8.out ? ZI_EPILOGUE_Y8 : 0) | (e.y8.turned ? ZI_EPILOGUE_TURNED : 0));
+    const int outputs8 = (e.y8.out ? ZI_EPILOGUE_Y8 : 0) | (e.y8.turned ? ZI_EPILOGUE_TURNED : 0);
+    if (e.z && !e.y && outputs8 && fp8_matmul_z_first(a.m, a.n, a.k, outputs8)) return launch_z_first(a, e, dtype, s);
+    const EpiloguePlan p = plan_fp8_matmul_epilogue(a.m, a.n, a.k, outputs8);
     if (!p.whole) {
         const hipError_t err = launch_sums(a, p.plan, workspace, s);
         if (err != hipSuccess) return err;
         return launch_epilogue(e, EpilogueSource{nullptr, 0, workspace, p.plan.parts}, dtype, s);
     }
-    if (p.plan.shape >= kAlone && e.z && !e.y && (e.y8.out || e.y8.turned)) return launch_z_first(a, p.plan, e, dtype, s);
     if (p.plan.shape == kFewRows) return dtype == ZI_BF16 ? launch_few_epilogue<ZI_BF16>(a, e, s) : launch_few_epilogue<ZI_FP16>(a, e, s);
     switch (kind_of(e.activation)) {
     case ActivationKind::kFloor: return launch_fp8_matmul_epilogue_tiles<ActivationKind::kFloor>(a, p.plan, e, dtype, s);

@@ -5,7 +5,7 @@ import torch
 
 import paper_2104_07857_amd as zi
 from epilogue_util import ACTIVATIONS, HALF_ULP, LEAST, OFFSET, SEED, act, dropped, factor, kept, near, near8, same8
-from epilogue_plans import SUMS, of_rounded_z
+from epilogue_plans import ALONE, SUMS, of_rounded_z
 from fp8_plans import FEW_16, FEW_32, PARTS, TILES
 from fp8_util import DT, Matrix, normal, numbers, quantized, same, view_of
 from test_gpu_epilogue import _empty, _is_quantised, _whole
@@ -61,7 +61,7 @@ def _want(product, activation, drop, bias, residual):
     return z, y if residual is None else y + residual.double()
 
 
-ALL = FEW_16 + FEW_32 + PARTS + TILES + SUMS
+ALL = FEW_16 + FEW_32 + PARTS + TILES + SUMS + ALONE
 
 
 @pytest.mark.parametrize("m,n,k", ALL)
@@ -88,7 +88,7 @@ def test_whole_numbers_are_exact(m, n, k, dtype):
     assert torch.equal(inplace, _want(product, "none", 0.5, bias, residual)[1].to(dtype))
 
 
-@pytest.mark.parametrize("m,n,k", [FEW_16[1], FEW_16[3], FEW_32[0], PARTS[1], PARTS[5], TILES[0], TILES[5], TILES[7], TILES[9], TILES[12], TILES[16]])
+@pytest.mark.parametrize("m,n,k", [FEW_16[1], FEW_16[3], FEW_32[0], PARTS[1], PARTS[5], TILES[0], TILES[5], TILES[7], TILES[9], TILES[12], TILES[16]] + ALONE)
 @pytest.mark.parametrize("dtype", HALF)
 @pytest.mark.parametrize("activation", list(ACTIVATIONS))
 def test_normal_numbers_within_the_bounds(m, n, k, dtype, activation):
@@ -113,7 +113,7 @@ def test_normal_numbers_within_the_bounds(m, n, k, dtype, activation):
         assert float((p.y8.values() - exact8).norm() / y.norm()) <= 0.01
 
 
-@pytest.mark.parametrize("m,n,k", [s for s in TILES if of_rounded_z(*s, "z,y8,turned")][::2])
+@pytest.mark.parametrize("m,n,k", [s for s in TILES + ALONE if of_rounded_z(*s, "z,y8,turned")])
 @pytest.mark.parametrize("dtype", HALF)
 @pytest.mark.parametrize("activation", ["none", "gelu", "silu"])
 def test_what_is_made_of_the_rounded_z(m, n, k, dtype, activation):
@@ -141,7 +141,7 @@ def test_what_is_made_of_the_rounded_z(m, n, k, dtype, activation):
         assert p.turned is None or near8(p.turned, y.t().contiguous(), off.t().contiguous())
 
 
-@pytest.mark.parametrize("m,n,k", [FEW_16[3], FEW_32[2], PARTS[1], TILES[0], TILES[9], TILES[16]])
+@pytest.mark.parametrize("m,n,k", [FEW_16[3], FEW_32[2], PARTS[1], TILES[0], TILES[9], TILES[16]] + ALONE)
 def test_nan_keeps_to_its_place(m, n, k):
     """A NaN in an operand makes NaN of a row, and no more in any output; what is dropped of it is 0."""
     a, b = _whole8(m, k, 1, 9), _whole8(n, k, 1, 10)
@@ -156,7 +156,7 @@ def test_nan_keeps_to_its_place(m, n, k):
     assert torch.equal(p.y8.scales(), scales) and same(numbers(p.y8.codes()), codes)
 
 
-@pytest.mark.parametrize("m,n,k", [FEW_16[3], PARTS[1], TILES[3], TILES[7], TILES[8], TILES[9], TILES[11], TILES[12], TILES[16]])
+@pytest.mark.parametrize("m,n,k", [FEW_16[3], PARTS[1], TILES[3], TILES[7], TILES[8], TILES[9], TILES[11], TILES[12], TILES[16]] + ALONE)
 def test_infinities_have_no_part_in_a_scale(m, n, k):
     """A row of A whose products pass what fp32 holds: infinities in its row of y, NaN in 8 bits, and the scales of its columns' blocks those of the other rows."""
     a, b = _whole8(m, k, 1, 20), _whole8(n, k, 1, 21)
@@ -186,7 +186,7 @@ def test_k_of_zero(m, n):
     assert torch.equal(y.double(), want) and _is_quantised(y8, want) and _is_quantised(turned, want.t())
 
 
-@pytest.mark.parametrize("m,n,k", [FEW_16[1], FEW_32[0], PARTS[1], TILES[0], TILES[8], TILES[9], TILES[16]])
+@pytest.mark.parametrize("m,n,k", [FEW_16[1], FEW_32[0], PARTS[1], TILES[0], TILES[8], TILES[9], TILES[16]] + ALONE)
 def test_same_bits_every_time_on_any_stream_and_in_a_graph(m, n, k):
     a, b = _normal(m, k, 1, 12), _normal(n, k, 128, 13)
     bias, residual = normal((n,), 14, 0.5, torch.bfloat16), normal((m, n), 15, 2.0, torch.bfloat16)
