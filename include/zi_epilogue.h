@@ -11,8 +11,7 @@
  *   z = x + bias             y = residual + drop(act(z))
  *
  * in fp32, each output rounded once from there: z and y to dtype, y8 and its transpose `turned` to 8 bits as zi_fp8_quantize does (block_rows 1: blocks of
- * 128 columns of y, and of 128 rows of y).  y is made of the unrounded z; but where zi_fp8_matmul_epilogue has z and outputs in 8 bits to write and no y in 16 bits, these may be made of
- * the rounded one, which the backward pass reads too (an infinity of its type becomes NaN in them).
+ * 128 columns of y, and of 128 rows of y).  y is made of the unrounded z.
  *
  *   ZI_ACT_NONE       z
  *   ZI_ACT_RELU       0 where z < 0, else z

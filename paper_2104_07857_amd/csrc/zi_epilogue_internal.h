@@ -41,7 +41,6 @@ struct EpiloguePlan {
     int32_t whole;                // all outputs come from the product's kernel; else a second one makes them of its sums
 };
 EpiloguePlan plan_fp8_matmul_epilogue(int64_t m, int64_t n, int64_t k, int outputs8);
-bool fp8_matmul_z_first(int64_t m, int64_t n, int64_t k, int outputs8);      // what is in 8 bits is made of z as it was written, if that is wanted and y is not
 size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int outputs8);
 hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpilogueArgs& e, int dtype, float* workspace, hipStream_t s);
 

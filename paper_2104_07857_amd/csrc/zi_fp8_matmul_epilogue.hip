@@ -128,45 +128,15 @@ EpiloguePlan plan_fp8_matmul_epilogue(int64_t m, int64_t n, int64_t k, int outpu
     return {plan, 0};
 }
 
-// Where z goes out and y does not in 16 bits (which would else be rounded twice; what is in 8 bits is rounded 16 times as far), large products leave z first, in the fastest tiles for that, and what
-// is in 8 bits is made of it by a kernel that reads it again.  us, one kernel in 128 x 128 / two, with gelu, 8 bits both ways: 8191 x 8192 x 2048 194 / 175, 4096 x 16384 x 4096 306 / 259, 8192 x
-// 32768 x 8192 2175 / 1758 (in 256 x 256 252, 339 and 2026), without an activation 175 / 164, 285 / 250, 2084 / 1728; but 2048 x 8192 x 2048 49 / 52, and to 8 bits along the rows 39 / 45
-// without an activation and 1500 x 16384 x 4096 101 / 105.
-static constexpr float kZOut = 0.2e-6f, kZStream = 7.5e6f;       // us an element that z takes beside each of the others; bytes a us of the second kernel, which finds some of z in the caches
-bool fp8_matmul_z_first(int64_t m, int64_t n, int64_t k, int outputs8)
-{
-    float any, whole;
-    if (plan_fp8_matmul_from(m, n, k, kFewRows, MatmulAlone{}, any).shape < kAloneShape) return false;
-    plan_whole(m, n, k, outputs8, whole);
-    const float cells = (float)m * (float)n, out = (outputs8 & ZI_EPILOGUE_Y8 ? 1.0f : 0.0f) + (outputs8 & ZI_EPILOGUE_TURNED ? 1.0f : 0.0f);
-    return any + kSecond + (2.0f + out) * cells / kZStream < whole + kZOut * out * cells;
-}
-
 size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int outputs8)
 {
     const EpiloguePlan p = plan_fp8_matmul_epilogue(m, n, k, outputs8);
     return p.whole ? 0 : p.plan.parts * (size_t)m * (size_t)n;
 }
 
-static hipError_t launch_z_first(const MatmulArgs& a, const EpilogueArgs& e, int dtype, hipStream_t s)
-{
-    EpilogueArgs first = e, then = e;
-    first.residual = nullptr;
-    first.drop = DropoutArgs{};
-    first.activation = ZI_ACT_NONE;
-    first.y8 = QuantizeArgs{};
-    const hipError_t err = launch_fp8_matmul_epilogue_tiles<ActivationKind::kFloor>(a, plan_fp8_matmul(a.m, a.n, a.k), first, dtype, s);
-    if (err != hipSuccess) return err;
-    then.bias = nullptr;
-    then.z = nullptr;
-    return launch_epilogue(then, EpilogueSource{e.z, e.z_ld, nullptr, 0}, dtype, s);
-}
-
 hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpilogueArgs& e, int dtype, float* workspace, hipStream_t s)
 {
-    const int outputs8 = (e.y8.out ? ZI_EPILOGUE_Y8 : 0) | (e.y8.turned ? ZI_EPILOGUE_TURNED : 0);
-    if (e.z && !e.y && outputs8 && fp8_matmul_z_first(a.m, a.n, a.k, outputs8)) return launch_z_first(a, e, dtype, s);
-    const EpiloguePlan p = plan_fp8_matmul_epilogue(a.m, a.n, a.k, outputs8);
+    const EpiloguePlan p = plan_fp8_matmul_epilogue(a.m, a.n, a.k, (e.y8.out ? ZI_EPILOGUE_Y8 : 0) | (e.y8.turned ? ZI_EPILOGUE_TURNED : 0));
     if (!p.whole) {
         const hipError_t err = launch_sums(a, p.plan, workspace, s);
         if (err != hipSuccess) return err;

@@ -16,15 +16,6 @@ def plan(m, n, k, outputs8):
     return f(m, n, k, outputs8)
 
 
-def of_rounded_z(m, n, k, outputs):
-    """Whether outputs in 8 bits are made of z as it was written, by a second kernel: in large products, where y is not wanted in 16 bits."""
-    wanted = outputs.split(",")
-    outputs8 = ("y8" in wanted) * Y8 + ("turned" in wanted) * TURNED
-    f = ctypes.CDLL(zi.LIB_PATH)._ZN2zi18fp8_matmul_z_firstEllli
-    f.restype, f.argtypes = ctypes.c_bool, [ctypes.c_int64] * 3 + [ctypes.c_int]
-    return "z" in wanted and "y" not in wanted and outputs8 > 0 and f(m, n, k, outputs8)
-
-
 # sums of tiles of 64 x 128, of which a second kernel makes the transposed numbers
 SUMS = [(320, 6050, 8001), (300, 5003, 6100)]
 # outputs in 8 bits from tiles of 256 x 256 and of 256 x 128

@@ -5,7 +5,7 @@ import random
 import pytest
 
 import paper_2104_07857_amd as zi
-from epilogue_plans import ALONE, BOTH, SUMS, TURNED, Y8, of_rounded_z, plan
+from epilogue_plans import ALONE, BOTH, SUMS, TURNED, Y8, plan
 from fp8_plans import FEW, FEW_16, FEW_32, PARTS, SHAPES, TILES
 from fp8_plans import plan as product_plan
 
@@ -48,15 +48,3 @@ def test_without_8_bit_outputs_it_is_the_products_own_way():
     for s in ALL:
         p, q = plan(*s, 0), product_plan(*s)
         assert (p.shape, p.parts, p.part_steps) == (q.shape, q.parts, q.part_steps)
-
-
-def test_z_is_first_only_where_all_comes_from_tiles():
-    """Then no workspace is asked for; the sizes of the GPU tests go both ways, and no call does that wants y in 16 bits."""
-    r = random.Random(4)
-    for s in ALL + [tuple(int(2 ** r.uniform(lo, 15)) for lo in (4, 4, 4)) for _ in range(20000)]:
-        for outputs, outputs8 in (("z,y8", Y8), ("z,turned", TURNED), ("z,y8,turned", BOTH)):
-            if of_rounded_z(*s, outputs):
-                assert plan(*s, outputs8).whole == 1 and zi.zi_fp8_matmul_epilogue_workspace_bytes(*s, outputs8) == 0 and product_plan(*s).shape >= 4, s
-        assert not of_rounded_z(*s, "z,y,y8,turned") and not of_rounded_z(*s, "y8,turned")
-    ways = {of_rounded_z(*s, "z,y8,turned") for s in ALL if product_plan(*s).shape >= 4}
-    assert ways == {False, True}
