@@ -17,9 +17,11 @@ LIB_PATH = os.path.join(HERE, "libzi.so")
 CALL_PATH = os.path.join(HERE, "_zi_call" + importlib.machinery.EXTENSION_SUFFIXES[0])
 SOURCES = ["zi_kernels.hip", "zi_api.hip", "zi_plan.hip", "zi_engine.hip", "zi_offload.hip", "zi_probe.hip",
            "zi_fp8_api.hip", "zi_fp8_rows.hip", "zi_fp8_matmul.hip",
-           "zi_epilogue_api.hip", "zi_epilogue_rows.hip", "zi_epilogue_tiles.hip", "zi_epilogue_backward.hip",
-           "zi_fp8_matmul_epilogue.hip",
-           "zi_fp8_matmul_floor.hip", "zi_fp8_matmul_sigmoid.hip", "zi_fp8_matmul_normal.hip"]
+           "zi_epilogue_api.hip", "zi_epilogue_plan.hip"]
+# The kernels of zi_epilogue.h, which libzi.so loads from its own folder when they are first called.
+EPILOGUE_PATH = os.path.join(HERE, "libzi_epilogue.so")
+EPILOGUE_SOURCES = ["zi_epilogue_rows.hip", "zi_epilogue_tiles.hip", "zi_epilogue_backward.hip", "zi_fp8_matmul_epilogue.hip",
+                    "zi_fp8_matmul_floor.hip", "zi_fp8_matmul_sigmoid.hip", "zi_fp8_matmul_normal.hip"]
 
 # -ffp-contract=off: the only fused multiply-adds are the ones the kernels write as fma.
 # Packed fp32 instructions are switched off for the device code.
@@ -48,7 +50,7 @@ def call_can_be_built() -> bool:
 
 
 def needs_build() -> bool:
-    built = [LIB_PATH, CALL_PATH] if call_can_be_built() else [LIB_PATH]
+    built = [LIB_PATH, EPILOGUE_PATH, CALL_PATH] if call_can_be_built() else [LIB_PATH, EPILOGUE_PATH]
     if not all(os.path.exists(f) for f in built):
         return True
     t = min(os.path.getmtime(f) for f in built)
@@ -110,15 +112,18 @@ def build(force: bool = True, extra_flags=(), out: str | None = None) -> str:
         subprocess.run(["g++", *HOST_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", os.path.join(CSRC, src),
                         "-o", obj], check=True)
         objs.append(obj)
-    # A source a process, as many as there are CPUs (16 at most); each leaves an object of its own next to the library that is made of them.
+    # A source a process, as many as there are CPUs (16 at most); each leaves an object of its own next to the libraries that are made of them.
     flags = [*HIPCC_FLAGS, *extra_flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     stem = os.path.splitext(out)[0]
-    hip_objs = [f"{stem}_{os.path.splitext(src)[0]}.o" for src in SOURCES]
-    compiles = [[hipcc(), *(f for f in flags if f != "-shared"), "-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, hip_objs)]
+    obj_of = {src: f"{stem}_{os.path.splitext(src)[0]}.o" for src in EPILOGUE_SOURCES + SOURCES}
+    compiles = [[hipcc(), *(f for f in flags if f != "-shared"), "-c", os.path.join(CSRC, src), "-o", obj] for src, obj in obj_of.items()]
     with concurrent.futures.ThreadPoolExecutor(max(1, min(16, os.cpu_count() or 1))) as pool:
         list(pool.map(_run_hipcc, compiles))
-    _run_hipcc([hipcc(), "--offload-arch=gfx950", "-shared", "-o", out, *hip_objs, *objs, "-pthread"])
-    for obj in hip_objs:
+    link = [hipcc(), "--offload-arch=gfx950", "-shared", "-pthread", "-o"]
+    _run_hipcc([*link, out, *(obj_of[s] for s in SOURCES), *objs])
+    # (both libraries have some kernels of the product: each takes its own)
+    _run_hipcc([*link, os.path.join(os.path.dirname(out), os.path.basename(EPILOGUE_PATH)), "-Wl,-Bsymbolic", *(obj_of[s] for s in EPILOGUE_SOURCES)])
+    for obj in obj_of.values():
         os.remove(obj)
     return out
 

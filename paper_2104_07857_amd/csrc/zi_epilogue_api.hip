@@ -1,5 +1,9 @@
 // C-ABI entry points of what follows a product: argument checks and launches.  See include/zi_epilogue.h for the contract.
+#include <dlfcn.h>
 #include <hip/hip_runtime.h>
+
+#include <cstdio>
+#include <cstring>
 
 #include "zi_epilogue_internal.h"
 #include "zi_fp8_checks.h"
@@ -119,6 +123,27 @@ zi::EpilogueArgs epilogue(const zi_epilogue_args& a, const zi_fp8_matrix* y8, co
     return e;
 }
 
+// The kernels' library, from the folder of this one; loaded once.
+const zi::EpilogueKernels* load_kernels()
+{
+    Dl_info self;
+    char at[4096] = "libzi_epilogue.so";
+    if (dladdr((const void*)&load_kernels, &self) && self.dli_fname) {
+        const char* slash = strrchr(self.dli_fname, '/');
+        const int length = slash ? (int)(slash + 1 - self.dli_fname) : 0;
+        if (snprintf(at, sizeof at, "%.*slibzi_epilogue.so", length, self.dli_fname) >= (int)sizeof at) return nullptr;
+    }
+    void* library = dlopen(at, RTLD_NOW | RTLD_LOCAL);
+    const auto get = library ? (const zi::EpilogueKernels* (*)())dlsym(library, "zi_epilogue_kernels") : nullptr;
+    return get ? get() : nullptr;
+}
+zi_status take_kernels(const zi::EpilogueKernels*& kernels)
+{
+    static const zi::EpilogueKernels* const loaded = load_kernels();
+    kernels = loaded;
+    return loaded ? ZI_OK : fail(ZI_ERR_HIP, "libzi_epilogue.so is not beside libzi.so, or cannot be loaded");
+}
+
 }  // namespace
 
 extern "C" zi_status zi_epilogue(const void* x, int64_t rows, int64_t cols, int64_t ld, const zi_epilogue_args* args, const zi_fp8_matrix* y8,
@@ -135,7 +160,9 @@ extern "C" zi_status zi_epilogue(const void* x, int64_t rows, int64_t cols, int6
     const int at = all.add("x", x, rows, cols * 2, ld * 2, false);
     add_epilogue(all, *args, y8, turned, rows, cols, 1u << at);
     if (zi_status st = all.check()) return st;
-    ZI_HIP(zi::launch_epilogue(epilogue(*args, y8, turned, rows, cols), zi::EpilogueSource{x, ld, nullptr, 0}, args->dtype, (hipStream_t)hip_stream));
+    const zi::EpilogueKernels* kernels;
+    if (zi_status st = take_kernels(kernels)) return st;
+    ZI_HIP(kernels->epilogue(epilogue(*args, y8, turned, rows, cols), zi::EpilogueSource{x, ld, nullptr, 0}, args->dtype, (hipStream_t)hip_stream));
     return ZI_OK;
 }
 
@@ -155,7 +182,8 @@ extern "C" zi_status zi_fp8_matmul_epilogue(const zi_fp8_matrix* a, const zi_fp8
     if (m == 0 || n == 0) return ZI_OK;
     if (zi_status st = check_epilogue_rows(*args, m, n)) return st;
     if (zi_status st = check_product_size(*a, *b)) return st;
-    const size_t wanted = zi_fp8_matmul_epilogue_workspace_bytes(m, n, k, (y8 ? ZI_EPILOGUE_Y8 : 0) | (turned ? ZI_EPILOGUE_TURNED : 0));
+    const int outputs8 = (y8 ? ZI_EPILOGUE_Y8 : 0) | (turned ? ZI_EPILOGUE_TURNED : 0);
+    const size_t wanted = zi_fp8_matmul_epilogue_workspace_bytes(m, n, k, outputs8);
     if (zi_status st = check_workspace(d_workspace, workspace_bytes, wanted)) return st;
     Arrays all;
     add_fp8(all, *a, "a's data", "a's scale", false);
@@ -163,7 +191,9 @@ extern "C" zi_status zi_fp8_matmul_epilogue(const zi_fp8_matrix* a, const zi_fp8
     add_epilogue(all, *args, y8, turned, m, n, 0);
     if (wanted > 0) all.add("d_workspace", d_workspace, 1, (int64_t)wanted, (int64_t)wanted, true);
     if (zi_status st = all.check()) return st;
-    ZI_HIP(zi::launch_fp8_matmul_epilogue(product(*a, *b), epilogue(*args, y8, turned, m, n), args->dtype, (float*)d_workspace, (hipStream_t)hip_stream));
+    const zi::EpilogueKernels* kernels;
+    if (zi_status st = take_kernels(kernels)) return st;
+    ZI_HIP(kernels->matmul(product(*a, *b), zi::plan_fp8_matmul_epilogue(m, n, k, outputs8), epilogue(*args, y8, turned, m, n), args->dtype, (float*)d_workspace, (hipStream_t)hip_stream));
     return ZI_OK;
 }
 
@@ -227,6 +257,12 @@ extern "C" zi_status zi_epilogue_backward(const zi_epilogue_backward_args* args,
     p.drop = dropout(a.drop, a.seed, a.offset, a.d_offset);
     p.activation = a.activation;
     p.dz8 = outputs8(dz8, turned, a.rows, a.cols);
-    ZI_HIP(zi::launch_epilogue_backward(p, a.dtype, (float*)d_workspace, (hipStream_t)hip_stream));
+    if (a.rows > 0) {
+        const zi::EpilogueKernels* kernels;
+        if (zi_status st = take_kernels(kernels)) return st;
+        ZI_HIP(kernels->backward(p, a.dtype, (float*)d_workspace, (hipStream_t)hip_stream));
+    }
+    if (a.dbias && (a.rows == 0 || a.rows > zi::kFp8Block))
+        ZI_HIP(zi::launch_column_sums((const float*)d_workspace, (int)up(a.rows, zi::kFp8Block), a.cols, a.dbias, a.dbias_dtype, a.accumulate, (hipStream_t)hip_stream));
     return ZI_OK;
 }

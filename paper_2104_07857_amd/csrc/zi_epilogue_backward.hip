@@ -105,14 +105,9 @@ hipError_t launch_epilogue_backward(const EpilogueBackwardArgs& given, int dtype
     const int64_t out = a.rows * a.cols * ((a.dz ? 2 : 0) + (a.dz8.out ? 1 : 0) + (a.dz8.turned ? 1 : 0));
     const bool large = a.rows * a.cols * (a.z ? 4 : 2) + out >= kLargeBytes;
     a.large_out = out >= kLargeOutBytes;
-    const int64_t down = (a.rows + kTile - 1) / kTile;
-    if (a.rows > 0) {
-        if (dtype == ZI_BF16) launch_backward_of<ZI_BF16>(a, large, partials, s);
-        else launch_backward_of<ZI_FP16>(a, large, partials, s);
-        const hipError_t err = hipGetLastError();
-        if (err != hipSuccess || down == 1) return err;
-    }
-    return a.dbias ? launch_column_sums(partials, (int)down, a.cols, a.dbias, a.dbias_dtype, a.accumulate, s) : hipSuccess;
+    if (dtype == ZI_BF16) launch_backward_of<ZI_BF16>(a, large, partials, s);
+    else launch_backward_of<ZI_FP16>(a, large, partials, s);
+    return hipGetLastError();
 }
 
 }  // namespace zi

@@ -42,7 +42,7 @@ struct EpiloguePlan {
 };
 EpiloguePlan plan_fp8_matmul_epilogue(int64_t m, int64_t n, int64_t k, int outputs8);
 size_t fp8_matmul_epilogue_workspace_floats(int64_t m, int64_t n, int64_t k, int outputs8);
-hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpilogueArgs& e, int dtype, float* workspace, hipStream_t s);
+hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpiloguePlan& p, const EpilogueArgs& e, int dtype, float* workspace, hipStream_t s);
 
 struct EpilogueBackwardArgs {
     int64_t rows, cols;
@@ -57,6 +57,14 @@ struct EpilogueBackwardArgs {
     QuantizeArgs dz8;
     bool large_out;
 };
-hipError_t launch_epilogue_backward(const EpilogueBackwardArgs& a, int dtype, float* workspace, hipStream_t s);
+// dz in all its forms, and dbias where there is but one row of tiles; of more of them their sums, in `partials`.
+hipError_t launch_epilogue_backward(const EpilogueBackwardArgs& a, int dtype, float* partials, hipStream_t s);
+
+// The kernels (260 of them) are a library of their own, libzi_epilogue.so beside libzi.so, which the first call that launches one loads: programs that only step do without.
+struct EpilogueKernels {
+    decltype(&launch_epilogue) epilogue;
+    decltype(&launch_fp8_matmul_epilogue) matmul;
+    decltype(&launch_epilogue_backward) backward;
+};
 
 }  // namespace zi
