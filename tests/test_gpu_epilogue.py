@@ -1,5 +1,8 @@
 """zi_epilogue and zi_epilogue_backward against their definitions in 64 bits (epilogue_util.py, which derives the tolerances).  Where numbers are small whole ones and the factor of dropout
 a power of two, results are exact and compared bit for bit, so that a wrong index, mask or scale cannot hide."""
+import ctypes
+import shutil
+
 import pytest
 import torch
 
@@ -9,6 +12,7 @@ from fp8_util import DT, Matrix, block_most, normal, quantized, same, view_of
 
 pytestmark = pytest.mark.gpu
 HALF = [torch.bfloat16, torch.float16]
+ZI_ERR_HIP = -4
 SIZES = [(1, 1), (1, 7), (3, 8), (2, 9), (5, 127), (1, 128), (7, 129), (16, 130), (17, 1000), (130, 257), (333, 1000), (128, 128), (129, 4100), (1, 16384), (2, 33001), (300, 640), (1025, 63)]
 
 
@@ -303,6 +307,19 @@ def test_no_rows():
         zi.zi_epilogue_backward(args)
         torch.cuda.synchronize()
         assert not bool(dbias.any())
+
+
+def test_without_the_library_of_its_kernels_a_call_is_an_error(tmp_path):
+    """libzi.so by itself, in a folder of its own: everything else works, and these calls say what is missing."""
+    alone = ctypes.CDLL(shutil.copy(zi.LIB_PATH, tmp_path))
+    x = torch.zeros((3, 16), dtype=torch.bfloat16, device="cuda:0")
+    args = zi.make_epilogue(3, 16, zi.ZI_BF16, y=x)
+    alone.zi_last_error.restype = ctypes.c_char_p
+    for _ in range(2):
+        assert alone.zi_epilogue(ctypes.c_void_p(x.data_ptr()), *map(ctypes.c_int64, (3, 16, 16)), ctypes.byref(args), None, None, None) == ZI_ERR_HIP
+        assert b"libzi_epilogue.so" in alone.zi_last_error()
+    torch.cuda.synchronize()
+    assert not bool(x.any())
 
 
 def test_matrices_of_more_than_four_gib():
