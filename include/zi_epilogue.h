@@ -87,8 +87,9 @@ zi_status zi_fp8_matmul_epilogue(const zi_fp8_matrix* a, const zi_fp8_matrix* b,
 
 /*
  *   dz = drop(dy) * act'(z)       dbias = sum over rows of dz
- * dz is the gradient of x as well; that of the residual is dy itself.  dy, z, dz: rows x cols in dtype with their own pitches; z (bias and all) is not read, and may be NULL, where activation is
- * ZI_ACT_NONE.  act' of ZI_ACT_RELU is 0 where z <= 0, else 1; where it is 0, dz is 0 whatever dy is.  dropout's arguments as the forward call had them.  dbias: cols in dbias_dtype (dtype
+ * An element that dropout drops has dz 0, whatever dy and z are there.  dz is the gradient of x as well; that of the residual is dy itself.  dy, z, dz: rows x cols in dtype with their own
+ * pitches; z (bias and all) is not read, and may be NULL, where activation is ZI_ACT_NONE.  act' of ZI_ACT_RELU is 0 where z <= 0, else 1; where it is 0, dz is 0 whatever dy is.
+ * dropout's arguments as the forward call had them.  dbias: cols in dbias_dtype (dtype
  * or ZI_FP32), or NULL; with accumulate != 0 it is added to, rounded once; the sum over rows is made in fp32, of the unrounded dz, in a fixed order.  dz8 (rows x cols) and turned
  * (cols x rows) are dz in 8 bits, with block_rows 1, of the unrounded dz.  dz, dbias, dz8 and turned are outputs, NULL where they are not wanted; at least one is.  dz may be dy or z in place.
  * d_workspace: as above, of at least zi_epilogue_workspace_bytes(rows, cols) bytes; may be NULL if dbias is.

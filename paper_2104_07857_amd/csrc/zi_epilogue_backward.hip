@@ -35,15 +35,18 @@ __global__ __launch_bounds__(256) void epilogue_backward_kernel(const EpilogueBa
             dy[i].template settle<ENDS>(at.left);
 #pragma unroll
             for (int j = 0; j < 8; ++j) dz[i][j] = dy[i].get(j);
-            drop.apply(dz[i], (uint32_t)(at.col >> 3), (uint32_t)row);
-            if constexpr (ACT != ZI_ACT_NONE) {
+            if constexpr (ACT == ZI_ACT_NONE) {
+                drop.apply(dz[i], (uint32_t)(at.col >> 3), (uint32_t)row);
+            } else {
+                float f[8] = {};
                 if (ACT != kAnyActivation || a.z) {
-                    float f[8];
                     z[i].template settle<ENDS>(at.left);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) f[j] = z[i].get(j);
-                    derive<ACT>(dz[i], f, a.activation);
                 }
+                if constexpr (ACT == ZI_ACT_RELU) drop.apply(dz[i], (uint32_t)(at.col >> 3), (uint32_t)row);       // (it leaves 0 at 0, whatever z is)
+                else drop.apply(dz[i], f, (uint32_t)(at.col >> 3), (uint32_t)row);
+                derive<ACT>(dz[i], f, a.activation);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += dz[i][j];

@@ -183,6 +183,18 @@ struct Dropout {
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = is_kept(w, j, threshold) ? x[j] * scale : 0.0f;
     }
+    // The same of a gradient that a derivative at z follows: what is dropped is made of z = 0, since 0 times the derivative at an infinity or NaN would not be 0.
+    __device__ __forceinline__ void apply(float (&x)[8], float (&z)[8], uint32_t octet, uint32_t row) const
+    {
+        if (!active()) return;
+        const u32x4 w = numbers(octet, row);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool keep = is_kept(w, j, threshold);
+            x[j] = keep ? x[j] * scale : 0.0f;
+            z[j] = keep ? z[j] : 0.0f;
+        }
+    }
 };
 
 }  // namespace zi
