@@ -20,8 +20,8 @@
  *   ZI_ACT_SILU       z / (1 + exp(-z))
  *
  * Where z is finite, act(z) is within 2^-16 of itself and 2^-118 besides, and its derivative within 2^-16 of itself and 2^-20 besides (the exponent of exp is rounded to 2^-22 of itself,
- * which is why large arguments have the larger errors).  A NaN stays one; minus infinity becomes NaN, except under ZI_ACT_NONE and ZI_ACT_RELU, and so does the derivative at either
- * infinity.
+ * which is why large arguments have the larger errors).  A NaN stays one; minus infinity becomes NaN, except under ZI_ACT_NONE and ZI_ACT_RELU.  The derivative at an infinity is its limit
+ * (1, at minus infinity 0 except under ZI_ACT_NONE), since a z that dtype cannot hold is stored as one.
  *
  * Dropout keeps or drops each element by a number of 16 bits from the counter-based generator Philox4x32-10 (J. Salmon, M. Moraes, R. Dror, D. Shaw: "Parallel
  * random numbers: as easy as 1, 2, 3", SC 2011): key (seed's low word, high word), counter (column / 8, row, low word and high word of the offset); of the four words that

@@ -49,7 +49,11 @@ __device__ __forceinline__ float activated(float z)
     } else if constexpr (ACT == ZI_ACT_SILU) return z * sigmoid_of_exponent(-kLog2E * z);
     else return z;
 }
-// dy times the derivative.  (Where a sigmoid s is 0 or 1, s (1 - s) is 0, which its large factors are multiplied to one after the other.)
+// dy times the derivative.  (Where a sigmoid s is 0 or 1, s (1 - s) is 0, which its large factors are multiplied to one after the other; z counts as FAR there at most, so that
+// infinities have the limits 0 and 1 and not 0 times infinity.  A NaN comes back through exp.)  It is one instruction an element.  us, without / with, to 8 bits both ways and dbias: gelu_tanh of
+// 8191 x 16384 155.9 / 156.0, gelu of 8192 x 16384 159.0 / 160.1, silu 154.0 / 154.2.
+template <int FAR>
+__device__ __forceinline__ float not_beyond(float z) { return __builtin_amdgcn_fmed3f(z, -(float)FAR, (float)FAR); }
 template <int ACT>
 __device__ __forceinline__ float with_derivative(float dy, float z)
 {
@@ -57,15 +61,15 @@ __device__ __forceinline__ float with_derivative(float dy, float z)
     else if constexpr (ACT == ZI_ACT_GELU) {
         float e;
         const float phi = normal_cdf(z, e);
-        return dy * __builtin_fmaf(z * e, 0.398942280f, phi);
+        return dy * __builtin_fmaf(not_beyond<64>(z) * e, 0.398942280f, phi);                                   // (beyond 15, e is 0)
     } else if constexpr (ACT == ZI_ACT_GELU_TANH) {
         // 1 - s is exp(..) s, without the rounding of s near 1, which the slope of the cube (up to 50) would make much of; 1 where exp is infinite.
         const float z2 = z * z, e = exp2_of(z * __builtin_fmaf(z2, -kLog2E * kTanhCube, -kLog2E * kTanh)), s = inverse(1.0f + e), rest = __builtin_fminf(e * s, 1.0f);
         const float slope = __builtin_fmaf(__builtin_fminf(z2, 256.0f), 3.0f * kTanhCube, kTanh);                // (beyond 16, s (1 - s) is 0)
-        return dy * __builtin_fmaf(s * rest * z, slope, s);
+        return dy * __builtin_fmaf(s * rest * not_beyond<16>(z), slope, s);
     } else if constexpr (ACT == ZI_ACT_SILU) {
         const float s = sigmoid_of_exponent(-kLog2E * z);
-        return dy * __builtin_fmaf(__builtin_fmaf(-s, s, s), z, s);
+        return dy * __builtin_fmaf(__builtin_fmaf(-s, s, s), not_beyond<128>(z), s);                            // (beyond 89, s is 0 or 1)
     } else return dy;
 }
 // f(activation as a type), for an activation that is the same in all lanes.

@@ -1,5 +1,5 @@
-"""zi_epilogue_backward where z or dy hold infinities and NaN: what dropout took out of y passes nothing back, whatever it was, in any form of dz and in
-dbias."""
+"""zi_epilogue_backward where z or dy hold infinities and NaN: what dropout took out of y passes nothing back, whatever it was; at an infinite z, which is what a z beyond 65504 is stored as in fp16
+though y is finite, the derivative is its limit; and in all forms of dz and in dbias nothing else is touched."""
 import pytest
 import torch
 
@@ -71,3 +71,33 @@ def test_what_is_dropped_has_no_gradient(rows, cols, dtype, activation):
     a = Backward(dy, z, activation, "dz,dz8,turned", p, dbias)
     assert not bool(a.dz[~keep].any())
     _check(a, dbias, want, _off(dy, z, activation, p))
+
+
+@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("activation", list(ACTIVATIONS))
+@pytest.mark.parametrize("p", [0.0, 0.5])
+def test_the_derivative_at_an_infinite_z_is_its_limit(rows, cols, dtype, activation, p):
+    """1 at plus infinity, 0 at minus infinity; a NaN in z is one in dz (but for what does not look at it), and so is an infinite dy times 0."""
+    dy, z = normal((rows, cols), 53, 1e-3, dtype), _sprinkle(normal((rows, cols), 54, 1.0, dtype), (INF, -INF, INF), 3)
+    for more_z, more_dy in (((), ()), ((NAN,), (INF, -INF, NAN))):
+        _sprinkle(z, more_z, 11)
+        _sprinkle(dy, more_dy, 4)                                      # (at an infinite z too)
+        d = dropped(dy.double(), p)
+        want = d * _limit(z.double(), activation)
+        if activation == "relu":                                       # 0 where the derivative is, whatever dy is
+            want = torch.where(z.double() <= 0, torch.zeros_like(d), d)
+        want = torch.where(kept(rows, cols, p, device="cuda:0"), want, torch.zeros_like(want))
+        dbias = torch.empty(cols, device="cuda:0")
+        _check(Backward(dy, z, activation, "dz,dz8,turned", p, dbias), dbias, want, _off(dy, z, activation, p))
+
+
+@pytest.mark.parametrize("activation", ["gelu", "gelu_tanh", "silu"])
+def test_the_derivative_of_far_numbers(activation):
+    """Up to the largest of bf16 (fp16's numbers are in test_activations_of_every_number), as near as anywhere."""
+    z = torch.cat([s * torch.logspace(0, 38.5, 4096, dtype=torch.float64, device="cuda:0") for s in (1.0, -1.0)]).to(torch.bfloat16).reshape(1, -1)
+    one, dbias = torch.ones_like(z), torch.empty(z.shape[1], device="cuda:0")
+    Backward(one, z, activation, "dbias", dbias=dbias)
+    slope = derivative(z.double(), activation)
+    assert bool(slope.isfinite().all())
+    assert bool(((dbias.double() - slope).abs() <= slope.abs() * 2.0 ** -16 + 2.0 ** -20).all())
