@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import concurrent.futures
+import hashlib
 import importlib.machinery
 import os
 import shutil
@@ -100,6 +101,16 @@ def _run_hipcc(cmd):
         sys.stderr.write(err + "\n")
 
 
+def build_number(flags) -> int:
+    """64 bits of all sources and flags: two libraries that have the same are of one build."""
+    h = hashlib.sha256("\0".join(flags).encode())
+    for folder in (CSRC, os.path.join(ROOT, "include")):
+        for name in sorted(n for n in os.listdir(folder) if n.endswith((".h", ".hip", ".c", ".cpp"))):
+            with open(os.path.join(folder, name), "rb") as f:
+                h.update(name.encode() + b"\0" + f.read() + b"\0")
+    return int.from_bytes(h.digest()[:8], "little")
+
+
 def build(force: bool = True, extra_flags=(), out: str | None = None) -> str:
     out = out or LIB_PATH
     if not force and out == LIB_PATH and not needs_build():
@@ -113,7 +124,7 @@ def build(force: bool = True, extra_flags=(), out: str | None = None) -> str:
                         "-o", obj], check=True)
         objs.append(obj)
     # A source a process, as many as there are CPUs (16 at most); each leaves an object of its own next to the libraries that are made of them.
-    flags = [*HIPCC_FLAGS, *extra_flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    flags = [*HIPCC_FLAGS, *extra_flags, f"-DZI_BUILD={build_number([*HIPCC_FLAGS, *extra_flags])}ull", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     stem = os.path.splitext(out)[0]
     obj_of = {src: f"{stem}_{os.path.splitext(src)[0]}.o" for src in EPILOGUE_SOURCES + SOURCES}
     compiles = [[hipcc(), *(f for f in flags if f != "-shared"), "-c", os.path.join(CSRC, src), "-o", obj] for src, obj in obj_of.items()]

@@ -141,7 +141,8 @@ zi_status take_kernels(const zi::EpilogueKernels*& kernels)
 {
     static const zi::EpilogueKernels* const loaded = load_kernels();
     kernels = loaded;
-    return loaded ? ZI_OK : fail(ZI_ERR_HIP, "libzi_epilogue.so is not beside libzi.so, or cannot be loaded");
+    if (!loaded) return fail(ZI_ERR_HIP, "libzi_epilogue.so is not beside libzi.so, or cannot be loaded");
+    return loaded->build == ZI_BUILD ? ZI_OK : fail(ZI_ERR_HIP, "libzi_epilogue.so is of another build than libzi.so");
 }
 
 }  // namespace

@@ -60,8 +60,13 @@ struct EpilogueBackwardArgs {
 // dz in all its forms, and dbias where there is but one row of tiles; of more of them their sums, in `partials`.
 hipError_t launch_epilogue_backward(const EpilogueBackwardArgs& a, int dtype, float* partials, hipStream_t s);
 
-// The kernels (260 of them) are a library of their own, libzi_epilogue.so beside libzi.so, which the first call that launches one loads: programs that only step do without.
+// The kernels (266 of them) are a library of their own, libzi_epilogue.so beside libzi.so, which the first call that launches one loads: programs that only step do without.  Both have to be of
+// one build, which a number made of all sources and flags says (build.py), since they hand each other the structures above as they are.
+#ifndef ZI_BUILD
+#define ZI_BUILD 0
+#endif
 struct EpilogueKernels {
+    uint64_t build;
     decltype(&launch_epilogue) epilogue;
     decltype(&launch_fp8_matmul_epilogue) matmul;
     decltype(&launch_epilogue_backward) backward;

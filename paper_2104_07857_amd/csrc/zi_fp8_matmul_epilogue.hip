@@ -121,6 +121,6 @@ hipError_t launch_fp8_matmul_epilogue(const MatmulArgs& a, const EpiloguePlan& p
 // What libzi.so takes this library's kernels by.
 extern "C" __attribute__((visibility("default"))) const zi::EpilogueKernels* zi_epilogue_kernels()
 {
-    static const zi::EpilogueKernels kernels = {zi::launch_epilogue, zi::launch_fp8_matmul_epilogue, zi::launch_epilogue_backward};
+    static const zi::EpilogueKernels kernels = {ZI_BUILD, zi::launch_epilogue, zi::launch_fp8_matmul_epilogue, zi::launch_epilogue_backward};
     return &kernels;
 }
