@@ -2,6 +2,7 @@
 #include <dlfcn.h>
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstdio>
 #include <cstring>
 
@@ -123,26 +124,29 @@ zi::EpilogueArgs epilogue(const zi_epilogue_args& a, const zi_fp8_matrix* y8, co
     return e;
 }
 
-// The kernels' library, from the folder of this one; loaded once.
-const zi::EpilogueKernels* load_kernels()
+// The kernels' library, from the folder of this one, in the first call that needs it (two at once load the same).  One that failed is tried again in the next call.
+zi_status take_kernels(const zi::EpilogueKernels*& kernels)
 {
+    static std::atomic<const zi::EpilogueKernels*> loaded{nullptr};
+    kernels = loaded.load(std::memory_order_acquire);
+    if (kernels) return ZI_OK;
     Dl_info self;
     char at[4096] = "libzi_epilogue.so";
-    if (dladdr((const void*)&load_kernels, &self) && self.dli_fname) {
+    if (dladdr((const void*)&take_kernels, &self) && self.dli_fname) {
         const char* slash = strrchr(self.dli_fname, '/');
         const int length = slash ? (int)(slash + 1 - self.dli_fname) : 0;
-        if (snprintf(at, sizeof at, "%.*slibzi_epilogue.so", length, self.dli_fname) >= (int)sizeof at) return nullptr;
+        if (snprintf(at, sizeof at, "%.*slibzi_epilogue.so", length, self.dli_fname) >= (int)sizeof at) return fail(ZI_ERR_HIP, "the path of libzi_epilogue.so is too long");
     }
     void* library = dlopen(at, RTLD_NOW | RTLD_LOCAL);
     const auto get = library ? (const zi::EpilogueKernels* (*)())dlsym(library, "zi_epilogue_kernels") : nullptr;
-    return get ? get() : nullptr;
-}
-zi_status take_kernels(const zi::EpilogueKernels*& kernels)
-{
-    static const zi::EpilogueKernels* const loaded = load_kernels();
-    kernels = loaded;
-    if (!loaded) return fail(ZI_ERR_HIP, "libzi_epilogue.so is not beside libzi.so, or cannot be loaded");
-    return loaded->build == ZI_BUILD ? ZI_OK : fail(ZI_ERR_HIP, "libzi_epilogue.so is of another build than libzi.so");
+    if (!get) {
+        const char* why = dlerror();
+        return fail(ZI_ERR_HIP, "libzi_epilogue.so cannot be loaded: %s", why ? why : at);
+    }
+    kernels = get();
+    if (kernels->build != ZI_BUILD) return fail(ZI_ERR_HIP, "%s is of another build than libzi.so", at);
+    loaded.store(kernels, std::memory_order_release);
+    return ZI_OK;
 }
 
 }  // namespace

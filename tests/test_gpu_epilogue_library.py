@@ -7,9 +7,10 @@ import pytest
 import torch
 
 import paper_2104_07857_amd as zi
+from paper_2104_07857_amd import build as zb
 
 pytestmark = pytest.mark.gpu
-ZI_ERR_HIP = -4
+OK, ZI_ERR_HIP = 0, -4
 
 
 def _relu(library, x):
@@ -44,3 +45,14 @@ def test_a_library_of_another_build_is_refused(tmp_path):
         status, said, y = _relu(other, _x())
         assert status == ZI_ERR_HIP and "libzi_epilogue.so" in said and "another build" in said, (status, said)
         assert bool((y == 7.0).all())
+
+
+def test_a_load_that_failed_is_tried_again(tmp_path):
+    """And it says what the loader said."""
+    other = ctypes.CDLL(shutil.copy(zi.LIB_PATH, tmp_path))
+    status, said, _ = _relu(other, _x())
+    assert status == ZI_ERR_HIP and str(tmp_path / "libzi_epilogue.so") in said and "No such file" in said, (status, said)
+    shutil.copy(zb.EPILOGUE_PATH, tmp_path)
+    status, said, y = _relu(other, _x())
+    assert status == OK, said
+    assert torch.equal(y, _x().clamp_min(0))
