@@ -19,8 +19,13 @@ CALL_PATH = os.path.join(HERE, "_zi_call" + importlib.machinery.EXTENSION_SUFFIX
 SOURCES = ["zi_kernels.hip", "zi_api.hip", "zi_plan.hip", "zi_engine.hip", "zi_offload.hip", "zi_probe.hip",
            "zi_fp8_api.hip", "zi_fp8_rows.hip", "zi_fp8_matmul.hip",
            "zi_epilogue_api.hip", "zi_epilogue_plan.hip"]
-# The kernels of zi_epilogue.h, which libzi.so loads from its own folder when they are first called.
-EPILOGUE_PATH = os.path.join(HERE, "libzi_epilogue.so")
+# The kernels of zi_epilogue.h, which libzi.so loads from its own folder when they are first called; a library of another name those of its own name.
+def epilogue_path(lib: str) -> str:
+    stem, end = os.path.splitext(lib)
+    return stem + "_epilogue" + end
+
+
+EPILOGUE_PATH = epilogue_path(LIB_PATH)
 EPILOGUE_SOURCES = ["zi_epilogue_rows.hip", "zi_epilogue_tiles.hip", "zi_epilogue_backward.hip", "zi_fp8_matmul_epilogue.hip",
                     "zi_fp8_matmul_floor.hip", "zi_fp8_matmul_sigmoid.hip", "zi_fp8_matmul_normal.hip"]
 
@@ -133,7 +138,7 @@ def build(force: bool = True, extra_flags=(), out: str | None = None) -> str:
     link = [hipcc(), "--offload-arch=gfx950", "-shared", "-pthread", "-o"]
     _run_hipcc([*link, out, *(obj_of[s] for s in SOURCES), *objs])
     # (both libraries have some kernels of the product: each takes its own)
-    _run_hipcc([*link, os.path.join(os.path.dirname(out), os.path.basename(EPILOGUE_PATH)), "-Wl,-Bsymbolic", *(obj_of[s] for s in EPILOGUE_SOURCES)])
+    _run_hipcc([*link, epilogue_path(out), "-Wl,-Bsymbolic", *(obj_of[s] for s in EPILOGUE_SOURCES)])
     for obj in obj_of.values():
         os.remove(obj)
     return out

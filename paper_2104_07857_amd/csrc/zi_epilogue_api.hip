@@ -130,18 +130,18 @@ zi_status take_kernels(const zi::EpilogueKernels*& kernels)
     static std::atomic<const zi::EpilogueKernels*> loaded{nullptr};
     kernels = loaded.load(std::memory_order_acquire);
     if (kernels) return ZI_OK;
+    // Of this library's own path .../NAME.so, .../NAME_epilogue.so: builds under several names in one folder each have their own.
     Dl_info self;
-    char at[4096] = "libzi_epilogue.so";
-    if (dladdr((const void*)&take_kernels, &self) && self.dli_fname) {
-        const char* slash = strrchr(self.dli_fname, '/');
-        const int length = slash ? (int)(slash + 1 - self.dli_fname) : 0;
-        if (snprintf(at, sizeof at, "%.*slibzi_epilogue.so", length, self.dli_fname) >= (int)sizeof at) return fail(ZI_ERR_HIP, "the path of libzi_epilogue.so is too long");
-    }
+    char at[4096];
+    const char* path = dladdr((const void*)&take_kernels, &self) && self.dli_fname ? self.dli_fname : "libzi.so";
+    const char *slash = strrchr(path, '/'), *end = path + strlen(path);
+    for (const char* dot = slash ? slash : path; (dot = strstr(dot, ".so")); ++dot) end = dot;
+    if (snprintf(at, sizeof at, "%.*s_epilogue%s", (int)(end - path), path, end) >= (int)sizeof at) return fail(ZI_ERR_HIP, "the path of the epilogues' kernels is too long");
     void* library = dlopen(at, RTLD_NOW | RTLD_LOCAL);
     const auto get = library ? (const zi::EpilogueKernels* (*)())dlsym(library, "zi_epilogue_kernels") : nullptr;
     if (!get) {
         const char* why = dlerror();
-        return fail(ZI_ERR_HIP, "libzi_epilogue.so cannot be loaded: %s", why ? why : at);
+        return fail(ZI_ERR_HIP, "the epilogues' kernels cannot be loaded: %s", why ? why : at);
     }
     kernels = get();
     if (kernels->build != ZI_BUILD) return fail(ZI_ERR_HIP, "%s is of another build than libzi.so", at);

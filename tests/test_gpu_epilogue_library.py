@@ -56,3 +56,14 @@ def test_a_load_that_failed_is_tried_again(tmp_path):
     status, said, y = _relu(other, _x())
     assert status == OK, said
     assert torch.equal(y, _x().clamp_min(0))
+
+
+def test_a_build_of_another_name_has_a_library_of_its_own(tmp_path):
+    """libzi_more.so loads libzi_more_epilogue.so, and not the one of libzi.so beside it."""
+    other = ctypes.CDLL(shutil.copy(zi.LIB_PATH, tmp_path / "libzi_more.so"))
+    shutil.copy(zb.EPILOGUE_PATH, tmp_path)
+    status, said, _ = _relu(other, _x())
+    assert status == ZI_ERR_HIP and "libzi_more_epilogue.so" in said, (status, said)
+    shutil.copy(zb.EPILOGUE_PATH, tmp_path / "libzi_more_epilogue.so")
+    status, said, y = _relu(other, _x())
+    assert status == OK and torch.equal(y, _x().clamp_min(0)), said
