@@ -30,7 +30,8 @@
  * seed and offset.  Rows are counted from the call's first one; calls that shall not share a mask have different offsets.  The offset is `offset` plus, if d_offset is given, the number at
  * d_offset (device memory), read when the kernels run: a program that replays a captured graph counts it on there.
  *
- * Conventions are those of zi_fp8.h.  The results of a call do not depend on the order in which the GPU runs its workgroups, but the bits of an element of a product may depend
+ * Conventions are those of zi_fp8.h.  The kernels of these calls are a library of their own, libzi_epilogue.so in the folder of libzi.so and of the same build, which a process' first call that
+ * launches one loads (a capture may hold that call; it takes some milliseconds more); ZI_ERR_HIP if it cannot.  The results of a call do not depend on the order in which the GPU runs its workgroups, but the bits of an element of a product may depend
  * on the sizes, as zi_fp8_matmul says, and on which outputs are wanted.
  */
 #ifndef ZI_EPILOGUE_H
