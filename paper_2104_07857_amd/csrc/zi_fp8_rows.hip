@@ -8,9 +8,11 @@ namespace zi {
 
 // ---- quantisation ---------------------------------------------------------------------------------------------
 
-// A workgroup takes a tile of 128 x 128, which holds whole blocks of every kind, so x is read once whatever is wanted; a thread has 8 x 8 elements in
-// registers.  16384 x 4096 fp32 in squares, both 73 us (403 MB, 5.5 TB/s); 8191 x 8192 bf16, blocks of rows, both 55 us (269 MB, 4.9 TB/s, with 6 MB
-// more of scales that were written in pieces); one row of 1000 3.7 us.
+// A workgroup takes a tile of 128 x 128, which holds whole blocks of every kind, so x is read once whatever is wanted.
+// A thread has 8 x 8 elements in registers; 16 threads (a row of lanes) have a tile's row, so the largest of a row's
+// block comes from its lanes and that of a column's block from the thread's own rows, two steps over lanes and four
+// wavefronts.  The transposed numbers pass through LDS, which makes rows of 128 bytes of them.  16384 x 4096 fp32 in squares, both 73 us (403 MB, 5.5 TB/s);
+// 8191 x 8192 bf16, blocks of rows, both 55 us (269 MB, 4.9 TB/s, with 6 MB more of scales that were written in pieces); one row of 1000 3.7 us.
 // LARGE: the outputs do not stay in the memory-side cache for whoever reads them next.  Their stores pass it by then.  us, ordinary / so: 32768 x 8192
 // fp32 in squares, both 316 / 287, 16384 x 8192 bf16 114 / 102; but quantisation and product of 4096 x 4096 (x 4096) 70 / 75.
 // Large outputs of fp32 keep to two workgroups on a compute unit, three where registers allow them: 16384 x 4096 in squares 72.8 / 77.1, 32768 x 8192 280 /
@@ -19,10 +21,17 @@ constexpr int64_t kLargeBytes = (int64_t)96 << 20;
 template <int DT, bool LARGE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, LARGE && DT == ZI_FP32 ? 2 : 8))) void fp8_quantize_kernel(const QuantizeArgs a)
 {
-    __shared__ TileSpace<DT> s_space;
-    const int t = threadIdx.x, o = t & 15, g = t >> 4;
+    __shared__ uint32_t s_col[4][kTile / 8 * Octet<DT>::kWords];
+    __shared__ uint32_t s_all[4];
+    __shared__ __align__(16) uint8_t s_turned[kTile * kTile];
+
+    const int t = threadIdx.x, o = t & 15, g = t >> 4, wave = t >> 6;
     int64_t tile_row, tile_col;
     place_of_tile(blockIdx.x, gridDim.x, a.tiles_across, tile_row, tile_col);
+    const auto put = [](auto x, auto* at) {
+        if constexpr (LARGE) __builtin_nontemporal_store(x, at);
+        else *at = x;
+    };
     const int64_t row0 = tile_row * kTile + g * 8, col0 = tile_col * kTile + o * 8;
     const int64_t left = a.cols - col0;
     const int in_row = left >= 8 ? 8 : left > 0 ? (int)left : 0, in_row_or_less = left >= 8 ? 8 : (int)left;
@@ -44,7 +53,79 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, LARGE &&
             for (int i = 0; i < 8; ++i) x[i].template settle<Ends::kMoved>(in_row_or_less);
         }
     }
-    quantize_tile<DT, LARGE>(a, x, tile_row, tile_col, s_space);
+
+    constexpr int kWords = Octet<DT>::kWords;
+    uint32_t row_most[8], col_most[kWords], most;
+    const auto look = [&](auto finite) {
+        most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t m[kWords];
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+                m[w] = magnitudes<DT, decltype(finite)::value>(x[i].w[w]);
+                col_most[w] = i == 0 ? m[w] : max_of_words<DT>(col_most[w], m[w]);
+            }
+#pragma unroll
+            for (int w = 1; w < kWords; ++w) m[0] = max_of_words<DT>(m[0], m[w]);
+            row_most[i] = larger<DT>(m[0]);
+            most = max_of(most, row_most[i]);
+        }
+    };
+    look(std::false_type());
+    if (most >= kInfinity<DT>) look(std::true_type());
+    const bool square = a.out_square || a.turned_square, columns = a.turned && !a.turned_square;
+    if (square) {
+        most = max_of_rows<ZI_FP32>(max_16(most));
+        if ((t & 63) == 0) s_all[wave] = most;
+    }
+    if (columns) {
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+            const uint32_t m = max_of_rows<DT>(col_most[w]);
+            if ((t & 63) < 16) s_col[wave][o * kWords + w] = m;
+        }
+    }
+    if (square || columns) __syncthreads();
+    uint32_t all = 127;
+    if (square) all = scale_byte(as_fp32<DT>(max_of(max_of(s_all[0], s_all[1]), max_of(s_all[2], s_all[3]))));
+
+    if (a.out) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t byte = a.out_square ? all : scale_byte(as_fp32<DT>(max_16(row_most[i])));
+            if (row0 + i >= a.rows || in_row == 0) continue;
+            put(eight_e4m3<DT>(x[i], scale_of(byte)), reinterpret_cast<u32x2*>(a.out + (row0 + i) * a.out_ld + col0));
+            if (!a.out_square && o == 0) a.out_scale[(row0 + i) * a.out_scale_ld + tile_col] = (uint8_t)byte;
+        }
+        if (a.out_square && t == 0) a.out_scale[tile_row * a.out_scale_ld + tile_col] = (uint8_t)all;
+    }
+    if (!a.turned) return;
+
+    // A column's 128 numbers are eight chunks of 16 bytes; chunk p of column c lies at p ^ (c / 8 % 8), so that the 16
+    // threads that write one row's octets reach different banks.
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = o * 8 + j;
+        uint32_t byte = all;
+        if (!a.turned_square) {
+            const int w = c * kWords / 8;
+            const uint32_t m = max_of_words<DT>(max_of_words<DT>(s_col[0][w], s_col[1][w]), max_of_words<DT>(s_col[2][w], s_col[3][w]));
+            byte = scale_byte(as_fp32<DT>(DT == ZI_FP32 ? m : c % 2 ? m >> 16 : m & 0xFFFFu));
+        }
+        *reinterpret_cast<u32x2*>(s_turned + c * kTile + (((g >> 1) ^ (o & 7)) << 4) + (g & 1) * 8) = eight_e4m3_down<DT>(x, j, scale_of(byte));
+        if (!a.turned_square && g == 0 && j < in_row) a.turned_scale[(col0 + j) * a.turned_scale_ld + tile_row] = (uint8_t)byte;
+    }
+    if (a.turned_square && t == 0) a.turned_scale[tile_col * a.turned_scale_ld + tile_row] = (uint8_t)all;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = i * 32 + (t >> 3), part = t & 7;
+        const int64_t col = tile_col * kTile + c, row = tile_row * kTile + part * 16;
+        if (col >= a.cols || row >= a.rows) continue;
+        put(*reinterpret_cast<const u32x4*>(s_turned + c * kTile + ((part ^ ((c >> 3) & 7)) << 4)),
+            reinterpret_cast<u32x4*>(a.turned + col * a.turned_ld + row));
+    }
 }
 
 template <int DT>
