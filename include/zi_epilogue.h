@@ -12,6 +12,9 @@
  *
  * in fp32, each output rounded once from there: z and y to dtype, y8 and its transpose `turned` to 8 bits as zi_fp8_quantize does (block_rows 1: blocks of
  * 128 columns of y, and of 128 rows of y).  y is made of the unrounded z.
+ * The sums of a product have the error that zi_fp8_matmul names, which a rounding to 16 bits hides and one to 8 bits does not: a result as near as that to a border between two numbers of 8 bits
+ * comes out as the other one, about one in 400 where one column of A in 64 is twenty times the others (1.1e-3 to 1.7e-3 of the values in the 2-norm, where the rounding itself is 2.6e-2), and
+ * one scale in 60000 is the next one.
  *
  *   ZI_ACT_NONE       z
  *   ZI_ACT_RELU       0 where z < 0, else z

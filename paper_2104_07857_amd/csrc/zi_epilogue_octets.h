@@ -61,7 +61,7 @@ struct EpilogueOctet {
         }
     }
 };
-// The other parts' sums, in their order, for octets of R rows: with few rows three parts at a time are under way (there are 2, 4, 8 or 16), with more two.
+// The other parts' sums, in their order, for octets of R rows: with few rows three parts at a time are under way (there may be any number from 1 to 16), with more two.
 template <int R, int APART, int DT, int ACT, Ends ENDS>
 __device__ __forceinline__ void add_parts(EpilogueOctet<DT, ACT, true, ENDS, false> (&x)[R], const EpilogueArgs& e, const EpilogueSource& from, int64_t row0, int64_t col, int left)
 {

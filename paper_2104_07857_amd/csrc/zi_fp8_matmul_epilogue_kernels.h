@@ -139,7 +139,7 @@ enum class TileOutputs { k16, k8, k8AndZ };
 // in fp32 registers until its blocks' scales are known, which wavefronts side by side (FN 2) or below each other (FM 2) find together.  The product is the bound, and the epilogue what
 // nothing hides: with 256 rows a tile has a compute unit to itself.  us, product in 16 bits alone / bias, SiLU and y in 8 bits: 8192 x 32768 x 8192 (256 x 256) 1640 / 1690 to 1750, 1001 x 8192 x
 // 2048 (128 x 128, two on a compute unit) 20 / 24.  8191 x 4096 x 16384 with bias, dropout and residual 434 to 457; with C alone 430 to 450.  The largest kernels that keep sums, bias, mask and
-// scales have 12 to 20 bytes of scratch memory a thread behind the main loop; strips of tiles for each XCD and starts at other times gained nothing.
+// scales have up to 40 bytes of scratch memory a thread behind the main loop; strips of tiles for each XCD and starts at other times gained nothing.
 template <int DT, int FM, int FN, int RING, TileOutputs OUTPUTS, ActivationKind KIND>
 __global__ __launch_bounds__(256, RING * (FM + FN) > 8 ? 1 : 2) void fp8_matmul_epilogue_kernel(const MatmulArgs p, const TileOrder order, const EpilogueArgs e)
 {
